@@ -43,7 +43,7 @@ typedef enum {
     SKV_ENOMEM = -4      /* workspace allocation failed */
 } skv_status;
 
-typedef enum { SKV_F32 = 0, SKV_BF16 = 1, SKV_FP8_E4M3 = 2 /* semantic-vector table only */ } skv_dtype;
+typedef enum { SKV_F32 = 0, SKV_BF16 = 1, SKV_FP8_E4M3 = 2 /* semantic-vector table only (skv_cache_* hold theirs in it without being told) */ } skv_dtype;
 
 typedef struct {
     int32_t n_layers;       /* L: leading dimension of the K/V pools and of the semantic-vector table */
@@ -313,6 +313,99 @@ int skv_decode_step_noalloc(const skv_desc* desc, void* hip_stream, int32_t laye
  * Errors: SKV_EINVAL (null / misaligned pointers, n_heads < 1), SKV_ECAPACITY (n_heads > max_batch * Hq). */
 int skv_merge_lse(skv_ctx* ctx, int32_t n_heads, const float* out_a, const float* lse_a, const float* out_b, const float* lse_b,
                   float* out, float* lse);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rotary positions.  A head's first `rot` elements form rot / 2 pairs; pair i of a row at position p turns by the angle p * inv_freq[i]:
+ *     (x, y) -> m * (x cos - y sin, y cos + x sin),   m = mscale
+ * `interleaved` == 0: pair i is (i, i + rot / 2);  1: (2 i, 2 i + 1).  The elements from `rot` on are copied.  Angles are formed and reduced to a turn in 64 bits
+ * (positions of 10^6 and more lose nothing), products are fp32, rounded once to kv_dtype.  Negated positions turn back: with m = 1 that is the inverse, with any m
+ * the transposed map (what a gradient goes through).
+ *
+ * skv_rotary_freqs fills a table of frequencies (host memory; the caller copies it to the device) and the factor m:
+ *     SKV_ROPE_PLAIN   f_i = base^(-2 i / rot), m = 1
+ *     SKV_ROPE_LINEAR  f_i / factor (position interpolation)
+ *     SKV_ROPE_NTK     base * factor^(rot / (rot - 2)) in base's place: the first frequency keeps its value, the last one is divided by factor (rot >= 4)
+ *     SKV_ROPE_TURNS   by the turns r_i = original * f_i / (2 pi) that a pair makes over the original context: f_i / factor where r_i <= low, f_i where
+ *                      r_i >= high, and (1 - g) f_i / factor + g f_i, g = (r_i - low) / (high - low), between
+ *     SKV_ROPE_YARN    (arxiv 2309.00071, with the ramp over the pairs' indexes): with d(r) = rot ln(original / (2 pi r)) / (2 ln base), a = max(floor(d(high)), 0) and
+ *                      z = min(ceil(d(low)), rot - 1), the ramp u_i = (i - a) / (z - a) within [0, 1] (a step from 0 to 1 behind a where z <= a), f_i u_i / factor + f_i (1 - u_i),
+ *                      m = 0.1 ln(factor) + 1
+ * host  inv_freq [rot / 2] double, mscale [1].   No GPU is touched.
+ * Errors: SKV_EINVAL (null pointers; rot odd, < 2 or > D; base <= 1; factor < 1 where it is used; TURNS, YARN: low <= 0, high <= low or original <= 0; values
+ * that are not finite; an unknown scaling).
+ *
+ * skv_rotary: n tokens, all their heads.
+ * q dev [n][Hq][D], k dev [n][Hkv][D] kv_dtype (either may be NULL, with its output: left out);  pos dev [n] int32;  inv_freq dev [rot / 2] double
+ * q_out, k_out: as q and k, which they may be themselves (no other overlap).  Asynchronous.
+ * Errors: SKV_EINVAL (null / misaligned pointers, neither q nor k, n < 0, rot odd, < 2 or > D, interleaved not 0 or 1, mscale not finite), SKV_ECAPACITY
+ * (n > max_tokens).  n == 0 is a no-op. */
+typedef enum { SKV_ROPE_PLAIN = 0, SKV_ROPE_LINEAR = 1, SKV_ROPE_NTK = 2, SKV_ROPE_TURNS = 3, SKV_ROPE_YARN = 4 } skv_rope_scaling;
+int skv_rotary_freqs(int32_t rot, double base, int32_t scaling, double factor, double low, double high, double original, double* inv_freq, float* mscale);
+int skv_rotary(skv_ctx* ctx, int32_t n, const void* q, const void* k, const int32_t* pos, const double* inv_freq, int32_t rot, int32_t interleaved, float mscale,
+               void* q_out, void* k_out);
+
+/* ---------------------------------------------------------------------------------------------
+ * A cache of K/V rows that grows and is held in 8 bits: E4M3 codes (as in skv_desc) with one fp32 scale for each block of `block` tokens (16, 32, 64 or 128) of a
+ * sequence and head; a code c stands for c * scale.
+ *     K, V              dev [L][Hkv][T_total][D] bytes
+ *     k_scale, v_scale  dev [L][Hkv][T_total / block + B] fp32 (integer division)
+ *     cu_tok            dev [B + 1]: sequence b has the rows cu_tok[b] .. cu_tok[b + 1] - 1 to itself, used from the first on.  Its block t (rows t * block .. of the
+ *                       sequence, so that no block has rows of two) has its scale at cu_tok[b] / block + b + t.
+ *     n_tok             dev [B][Hkv], 4-byte aligned (a slice of an array of all layers will do): rows in use of each sequence and head
+ *     acc               dev [L][Hkv][T_total] fp32: attention weight gathered by each row
+ * All calls on a cache pass the same B, T_total and block.  What cu_tok, n_tok, counts and lists say is cut to the rows that a sequence has, never followed out of
+ * the pool; rows that no call names are left as they were.
+ * Scales are powers of two: the smallest s >= 2^-100 with |x| <= 448 s for the finite x of a block (E4M3 is a floating format: a scale between two powers would gain
+ * nothing, and these divide exactly).  The code of x is x / s rounded to nearest even; what is not finite becomes NaN.
+ *
+ * skv_cache_append: n_new tokens of layer `layer` behind the rows in use.  Token cu_new[b] + i becomes row n_tok[b][h] + i of sequence b.  A block that has rows
+ * already keeps its scale or takes a larger one that the new rows need; its codes are then rounded again to that (to nearest even: exact for all but codes that become
+ * subnormal).  n_tok is read only: the caller adds the tokens afterwards.  Tokens that do not fit a sequence's rows are dropped.
+ * k, v dev [n_new][Hkv][D] kv_dtype;  cu_new dev [B + 1];  max_new >= the most tokens of a sequence (more are dropped)
+ * acc  dev or NULL: the new rows' gathered weights become 0.  Asynchronous.
+ * Errors: SKV_EINVAL (null / misaligned pointers, layer, B < 1, T_total < 1, n_new < 0, max_new < 0, block), SKV_ECAPACITY (B > max_batch, T_total or n_new > max_tokens).
+ * n_new == 0 or max_new == 0 is a no-op. */
+int skv_cache_append(skv_ctx* ctx, int32_t layer, int32_t B, const void* k, const void* v, int32_t n_new, const int32_t* cu_new, int32_t max_new,
+                     const int32_t* cu_tok, const int32_t* n_tok, void* K, void* V, float* k_scale, float* v_scale, int32_t T_total, int32_t block, float* acc);
+
+/* skv_cache_attend: Eq. 3 for one token per sequence over the cache of layer `layer`: over the rows in use (tok_idx NULL) or over listed ones, as skv_select
+ * writes them.  out and lse as in skv_attend (they merge with others by skv_merge_lse): no row gives out = 0, lse = -inf.  A NaN logit or one of +inf gives NaN in out and
+ * lse; a logit of -inf weighs nothing.  Logits, maxima, sums and the products with V are fp32, fp32 queries enter with all their bits; a weight enters the product with V with 16 of its bits
+ * (off by at most 2^-18 of itself).  Results repeat bit for bit.
+ * q dev [B][Hq][D] kv_dtype;  out dev [B][Hq][D] fp32;  lse dev [B][Hq] or NULL
+ * max_n    >= the largest n_tok (more are not read).  With tok_idx: n_tok counts the entries of a list
+ * tok_idx  dev [B][Hkv][max_n] or NULL: rows, counted from the sequence's first; an entry that is none of its rows is skipped, one that comes twice counts twice
+ * acc_out  dev [L][Hkv][T_total] or NULL: of every row in use, acc_out = decay * acc + the sum of its weights over the G query heads of its KV head (acc NULL: 0 for it).
+ *          acc and acc_out may be the same.  Not with tok_idx.
+ * work     dev scratch of at least skv_cache_attend_work_bytes(ctx, B, max_n, acc_out != NULL) bytes (caller-owned; nothing is kept in it between calls)
+ * Asynchronous: one launch, one more where the rows of a head are split over blocks, one for acc_out.
+ * Errors: SKV_EINVAL (null / misaligned pointers, layer, B < 1, T_total < 1, max_n < 0, block, acc_out with tok_idx, acc without acc_out, decay not within [0, 1],
+ * work too small), SKV_ECAPACITY (B > max_batch, T_total or max_n > max_tokens).  skv_cache_attend_work_bytes returns -1 for arguments the call would reject. */
+int64_t skv_cache_attend_work_bytes(const skv_ctx* ctx, int32_t B, int32_t max_n, int32_t weights);
+int skv_cache_attend(skv_ctx* ctx, int32_t layer, int32_t B, const void* q, const void* K, const void* V, const float* k_scale, const float* v_scale, int32_t T_total,
+                     int32_t block, const int32_t* cu_tok, const int32_t* n_tok, const int32_t* tok_idx, int32_t max_n, float* out, float* lse, const float* acc,
+                     float* acc_out, float decay, void* work, int64_t work_bytes);
+
+/* skv_cache_evict: which rows stay when every layer, sequence and head may hold `keep`.  With n = n_tok rows in use: all where n <= keep; else the first `sink`, the last
+ * `recent`, and of the others the keep - sink - recent with the largest acc (equal: the lower row first; -0 == +0; NaN last).  Unlike skv_retain's, the choice is
+ * each head's own.
+ * acc dev [L][Hkv][T_total];  n_tok dev [L][B][Hkv];  max_n >= the largest n_tok (rows behind are not looked at)
+ * keep_idx dev [L][B][Hkv][max(keep, 1)] rows that stay, ascending, counted from the sequence's first (entries past n_keep are not written: with n_keep, a list that skv_gather
+ *          and skv_cache_attend take, too);  n_keep dev [L][B][Hkv] = min(n, keep).  Asynchronous.
+ * Errors: SKV_EINVAL (null / misaligned pointers, B < 1, T_total < 1, max_n < 0, keep < 0, sink < 0, recent < 0, sink + recent > keep), SKV_ECAPACITY (B > max_batch, T_total
+ * or max_n > max_tokens).
+ *
+ * skv_cache_compact: row j of a head becomes its row keep_idx[j], j < n_keep, for all layers, with its gathered weight (acc and acc_out, both or neither).  A block's new scale is the
+ * largest that its rows had; codes of rows with a smaller one are rounded again as in skv_cache_append.  The outputs have the layout of the inputs, which they may be
+ * themselves, all of them (the list must then be ascending, as skv_cache_evict writes it); rows and scales behind n_keep are left as they were.  An entry that is
+ * none of the sequence's rows gives a row of zeros.  Asynchronous.
+ * Errors: SKV_EINVAL (null / misaligned pointers, B < 1, T_total < 1, block, keep < 0, acc without acc_out or the other way round, some outputs that are their inputs and some that are
+ * not), SKV_ECAPACITY (B > max_batch, T_total > max_tokens).  keep == 0 is a no-op. */
+int skv_cache_evict(skv_ctx* ctx, int32_t B, const float* acc, int32_t T_total, const int32_t* cu_tok, const int32_t* n_tok, int32_t max_n, int32_t keep, int32_t sink,
+                    int32_t recent, int32_t* keep_idx, int32_t* n_keep);
+int skv_cache_compact(skv_ctx* ctx, int32_t B, const void* K, const void* V, const float* k_scale, const float* v_scale, const float* acc, int32_t T_total, int32_t block,
+                      const int32_t* cu_tok, const int32_t* keep_idx, int32_t keep, const int32_t* n_keep, void* K_out, void* V_out, float* k_scale_out, float* v_scale_out,
+                      float* acc_out);
 
 #ifdef __cplusplus
 }

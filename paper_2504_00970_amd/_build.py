@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libsentencekv.so")
 # built by `python -m paper_2504_00970_amd._build --stamps`, loaded by `bench.py --phase-stamps`
 LIB_STAMPS = os.path.join(HERE, "libsentencekv_stamps.so")
 CALLS = os.path.join(HERE, "_calls.so")
-SOURCES = ["api.hip", "prefill.hip", "decode.hip", "retain.hip"]
+SOURCES = ["api.hip", "prefill.hip", "decode.hip", "retain.hip", "cache.hip"]
 HEADERS = [os.path.join(CSRC, "skv_internal.h"), os.path.join(CSRC, "skv_device.h"), os.path.join(CSRC, "skv_stamps.h"),
            os.path.join(INCLUDE, "sentencekv.h")]
 

@@ -20,6 +20,7 @@ from . import _build
 
 SKV_F32, SKV_BF16, SKV_FP8_E4M3 = 0, 1, 2
 SKV_OK, SKV_EINVAL, SKV_ECAPACITY, SKV_EHIP, SKV_ENOMEM = 0, -1, -2, -3, -4
+SKV_ROPE_PLAIN, SKV_ROPE_LINEAR, SKV_ROPE_NTK, SKV_ROPE_TURNS, SKV_ROPE_YARN = 0, 1, 2, 3, 4
 
 
 class SkvError(RuntimeError):
@@ -35,7 +36,7 @@ class _Desc(ctypes.Structure):
 
 _LIB = None
 _CALLS = None
-_vp, _i32, _int, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int, ctypes.c_int64
+_vp, _i32, _int, _i64, _f32, _f64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_double
 
 _SIGNATURES = {
     "skv_create": (_int, [ctypes.POINTER(_vp), ctypes.POINTER(_Desc), _vp]),
@@ -63,6 +64,14 @@ _SIGNATURES = {
                                _vp, _vp, _vp]),
     "skv_decode_step_noalloc": (_int, [ctypes.POINTER(_Desc), _vp, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp,
                                        _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "skv_rotary_freqs": (_int, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp]),
+    "skv_rotary": (_int, [_vp, _i32, _vp, _vp, _vp, _vp, _i32, _i32, _f32, _vp, _vp]),
+    "skv_cache_append": (_int, [_vp, _i32, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp]),
+    "skv_cache_attend_work_bytes": (_i64, [_vp, _i32, _i32, _i32]),
+    "skv_cache_attend": (_int, [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _f32, _vp,
+                                _i64]),
+    "skv_cache_evict": (_int, [_vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "skv_cache_compact": (_int, [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -84,7 +93,7 @@ class _CtypesCalls:
         def call(*args):
             if len(args) != len(kinds):
                 raise TypeError("wrong number of arguments")
-            return fn(*(_address(a) if k is _vp and i in (0, address) else _p(a) if k is _vp else _number(a)
+            return fn(*(_address(a) if k is _vp and i in (0, address) else _p(a) if k is _vp else _real(a) if k is _f32 else _number(a)
                         for i, (a, k) in enumerate(zip(args, kinds))))
         return call
 
@@ -99,6 +108,12 @@ def _number(a):
     if isinstance(a, torch.Tensor):
         raise TypeError("a number expected, got a tensor")
     return operator.index(a)
+
+
+def _real(a):
+    if isinstance(a, torch.Tensor):
+        raise TypeError("a number expected, got a tensor")
+    return float(a)
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -268,6 +283,41 @@ class Context:
     def merge_lse(self, n_heads: int, out_a, lse_a, out_b, lse_b, out, lse=None) -> None:
         _check(_CALLS.skv_merge_lse(self._handle, n_heads, out_a, lse_a, out_b, lse_b, out, lse),
                "skv_merge_lse")
+
+    # ---- rotary positions ----------------------------------------------------------------------------
+    def rotary(self, n: int, q, k, pos, inv_freq, rot: int, interleaved: bool, mscale: float, q_out, k_out) -> None:
+        _check(_CALLS.skv_rotary(self._handle, n, q, k, pos, inv_freq, rot, int(interleaved), mscale, q_out, k_out), "skv_rotary")
+
+    # ---- the growing cache in 8 bits ---------------------------------------------------------------------
+    def cache_append(self, layer: int, B: int, k, v, n_new: int, cu_new, max_new: int, cu_tok, n_tok, K, V, k_scale, v_scale, T_total: int,
+                     block: int, acc=None) -> None:
+        _check(_CALLS.skv_cache_append(self._handle, layer, B, k, v, n_new, cu_new, max_new, cu_tok, n_tok, K, V, k_scale, v_scale, T_total,
+                                       block, acc), "skv_cache_append")
+
+    def cache_attend_work_bytes(self, B: int, max_n: int, weights: bool = False) -> int:
+        return int(_lib().skv_cache_attend_work_bytes(self._h, B, max_n, 1 if weights else 0))
+
+    def cache_attend(self, layer: int, B: int, q, K, V, k_scale, v_scale, T_total: int, block: int, cu_tok, n_tok, tok_idx, max_n: int, out,
+                     lse, acc, acc_out, decay: float, work) -> None:
+        _check(_CALLS.skv_cache_attend(self._handle, layer, B, q, K, V, k_scale, v_scale, T_total, block, cu_tok, n_tok, tok_idx, max_n, out,
+                                       lse, acc, acc_out, decay, work, work.numel() * work.element_size()), "skv_cache_attend")
+
+    def cache_evict(self, B: int, acc, T_total: int, cu_tok, n_tok, max_n: int, keep: int, sink: int, recent: int, keep_idx, n_keep) -> None:
+        _check(_CALLS.skv_cache_evict(self._handle, B, acc, T_total, cu_tok, n_tok, max_n, keep, sink, recent, keep_idx, n_keep),
+               "skv_cache_evict")
+
+    def cache_compact(self, B: int, K, V, k_scale, v_scale, acc, T_total: int, block: int, cu_tok, keep_idx, keep: int, n_keep, K_out, V_out,
+                      k_scale_out, v_scale_out, acc_out) -> None:
+        _check(_CALLS.skv_cache_compact(self._handle, B, K, V, k_scale, v_scale, acc, T_total, block, cu_tok, keep_idx, keep, n_keep, K_out,
+                                        V_out, k_scale_out, v_scale_out, acc_out), "skv_cache_compact")
+
+
+def rotary_freqs(rot: int, base: float, scaling: int = SKV_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 32.0,
+                 original: float = 0.0):
+    """skv_rotary_freqs: (frequencies, a float64 tensor in host memory; mscale)."""
+    f, m = torch.empty(max(rot // 2, 1), dtype=torch.float64), ctypes.c_float()
+    _check(_lib().skv_rotary_freqs(rot, base, scaling, factor, low, high, original, f.data_ptr(), ctypes.addressof(m)), "skv_rotary_freqs")
+    return f, float(m.value)
 
 
 NOALLOC_SCRATCH_BYTES = 8 * 1024 * 1024

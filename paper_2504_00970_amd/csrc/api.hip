@@ -1,5 +1,6 @@
 // C ABI of libsentencekv: context management, host-side argument checks, and the launch sequence of
 // every entry point declared in sentencekv.h.  All checks run before anything touches the GPU.
+#include <cmath>
 #include <mutex>
 #include <new>
 
@@ -46,6 +47,10 @@ inline int64_t layer_elems(const Ctx& c, int64_t rows) { return (int64_t)c.d.n_k
 inline int elt_bytes(const Ctx& c) { return c.d.kv_dtype == SKV_BF16 ? 2 : 4; }
 inline int sv_bytes(const Ctx& c) { return c.d.semvec_dtype == SKV_BF16 ? 2 : c.d.semvec_dtype == SKV_FP8_E4M3 ? 1 : 4; }
 
+
+// ---- the 8-bit cache --------------------------------------------------------------------------------------------------
+inline bool aligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool cache_block(int32_t block) { return block == 16 || block == 32 || block == 64 || block == 128; }
 
 // ---- skv_segment's wait for the number of sentences ---------------------------------------------------------------------
 constexpr unsigned int kNoCount = 0xffffffffu;
@@ -617,6 +622,108 @@ int skv_merge_lse(skv_ctx* ctx, int32_t n_heads, const float* out_a, const float
     const int rc = check_ctx(ctx);
     if (rc != SKV_OK) return rc;
     return hip_status(skv::launch_merge_lse(&ctx->c, out_a, lse_a, out_b, lse_b, n_heads, out, lse));
+}
+
+int skv_rotary_freqs(int32_t rot, double base, int32_t scaling, double factor, double low, double high, double original, double* inv_freq, float* mscale) {
+    if (!inv_freq || !mscale || rot < 2 || rot % 2 != 0 || rot > skv::kHeadDim) return SKV_EINVAL;
+    if (!std::isfinite(base) || !(base > 1.0) || scaling < SKV_ROPE_PLAIN || scaling > SKV_ROPE_YARN) return SKV_EINVAL;
+    if (scaling != SKV_ROPE_PLAIN && (!std::isfinite(factor) || !(factor >= 1.0))) return SKV_EINVAL;
+    if (scaling == SKV_ROPE_NTK && rot < 4) return SKV_EINVAL;
+    const bool banded = scaling == SKV_ROPE_TURNS || scaling == SKV_ROPE_YARN;
+    if (banded && (!std::isfinite(low) || !std::isfinite(high) || !std::isfinite(original) || !(low > 0.0) || !(high > low) || !(original > 0.0))) return SKV_EINVAL;
+    constexpr double kTurn = 6.283185307179586477;
+    if (scaling == SKV_ROPE_NTK) base *= std::pow(factor, (double)rot / (rot - 2));
+    double a = 0.0, z = 0.0;
+    if (scaling == SKV_ROPE_YARN) {
+        const double per = rot / (2.0 * std::log(base));
+        a = std::fmax(std::floor(per * std::log(original / (kTurn * high))), 0.0);
+        z = std::fmin(std::ceil(per * std::log(original / (kTurn * low))), rot - 1.0);
+    }
+    for (int32_t i = 0; i < rot / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rot);
+        double keep = 1.0;                                    // the part of f that is not divided
+        if (scaling == SKV_ROPE_LINEAR) keep = 0.0;
+        if (scaling == SKV_ROPE_TURNS) keep = std::fmin(std::fmax((original * f / kTurn - low) / (high - low), 0.0), 1.0);
+        if (scaling == SKV_ROPE_YARN) keep = 1.0 - (z > a ? std::fmin(std::fmax((i - a) / (z - a), 0.0), 1.0) : i > a ? 1.0 : 0.0);
+        inv_freq[i] = scaling == SKV_ROPE_NTK ? f : keep * f + (keep < 1.0 ? (1.0 - keep) * (f / factor) : 0.0);
+    }
+    *mscale = scaling == SKV_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+    return SKV_OK;
+}
+
+int skv_rotary(skv_ctx* ctx, int32_t n, const void* q, const void* k, const int32_t* pos, const double* inv_freq, int32_t rot, int32_t interleaved, float mscale,
+               void* q_out, void* k_out) {
+    if (!ctx) return SKV_EINVAL;
+    if (n < 0 || rot < 2 || rot % 2 != 0 || rot > skv::kHeadDim || (interleaved != 0 && interleaved != 1) || !std::isfinite(mscale)) return SKV_EINVAL;
+    if ((!q && !k) || (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return SKV_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || bad_ptr(pos) || bad_ptr(inv_freq)) return SKV_EINVAL;
+    if (n > ctx->c.d.max_tokens) return SKV_ECAPACITY;
+    const int rc = check_ctx(ctx);
+    if (rc != SKV_OK) return rc;
+    return hip_status(skv::launch_rotary(&ctx->c, n, q, k, pos, inv_freq, rot, interleaved != 0, mscale, q_out, k_out));
+}
+
+int skv_cache_append(skv_ctx* ctx, int32_t layer, int32_t B, const void* k, const void* v, int32_t n_new, const int32_t* cu_new, int32_t max_new,
+                     const int32_t* cu_tok, const int32_t* n_tok, void* K, void* V, float* k_scale, float* v_scale, int32_t T_total, int32_t block, float* acc) {
+    if (!ctx) return SKV_EINVAL;
+    if (layer < 0 || layer >= ctx->c.d.n_layers || B < 1 || T_total < 1 || n_new < 0 || max_new < 0 || !cache_block(block)) return SKV_EINVAL;
+    if (bad_ptr(cu_new) || bad_ptr(cu_tok) || !aligned4(n_tok) || bad_ptr(K) || bad_ptr(V) || bad_ptr(k_scale) || bad_ptr(v_scale) || !aligned16(acc)) return SKV_EINVAL;
+    if (n_new > 0 && (bad_ptr(k) || bad_ptr(v))) return SKV_EINVAL;
+    if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens || n_new > ctx->c.d.max_tokens) return SKV_ECAPACITY;
+    const int rc = check_ctx(ctx);
+    if (rc != SKV_OK) return rc;
+    if (max_new > T_total) max_new = T_total;                 // no sequence takes more
+    return hip_status(skv::launch_cache_append(&ctx->c, layer, B, k, v, n_new, cu_new, max_new, cu_tok, n_tok, K, V, k_scale, v_scale, T_total, block, acc));
+}
+
+int64_t skv_cache_attend_work_bytes(const skv_ctx* ctx, int32_t B, int32_t max_n, int32_t weights) {
+    if (!ctx || B < 1 || max_n < 0 || B > ctx->c.d.max_batch || max_n > ctx->c.d.max_tokens || (weights != 0 && weights != 1)) return -1;
+    return skv::cache_attend_work_bytes(&ctx->c, B, max_n, weights != 0);
+}
+
+int skv_cache_attend(skv_ctx* ctx, int32_t layer, int32_t B, const void* q, const void* K, const void* V, const float* k_scale, const float* v_scale, int32_t T_total,
+                     int32_t block, const int32_t* cu_tok, const int32_t* n_tok, const int32_t* tok_idx, int32_t max_n, float* out, float* lse, const float* acc,
+                     float* acc_out, float decay, void* work, int64_t work_bytes) {
+    if (!ctx) return SKV_EINVAL;
+    if (layer < 0 || layer >= ctx->c.d.n_layers || B < 1 || T_total < 1 || max_n < 0 || !cache_block(block)) return SKV_EINVAL;
+    if (bad_ptr(q) || bad_ptr(K) || bad_ptr(V) || bad_ptr(k_scale) || bad_ptr(v_scale) || bad_ptr(cu_tok) || !aligned4(n_tok) || bad_ptr(out) || bad_ptr(work))
+        return SKV_EINVAL;
+    if (!aligned16(tok_idx) || !aligned16(lse) || !aligned16(acc) || !aligned16(acc_out)) return SKV_EINVAL;
+    if ((acc_out && tok_idx) || (acc && !acc_out) || !(decay >= 0.0f && decay <= 1.0f)) return SKV_EINVAL;
+    if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens || max_n > ctx->c.d.max_tokens) return SKV_ECAPACITY;
+    if (work_bytes < skv::cache_attend_work_bytes(&ctx->c, B, max_n, acc_out != nullptr)) return SKV_EINVAL;
+    const int rc = check_ctx(ctx);
+    if (rc != SKV_OK) return rc;
+    return hip_status(skv::launch_cache_attend(&ctx->c, layer, B, q, K, V, k_scale, v_scale, T_total, block, cu_tok, n_tok, tok_idx, max_n, out, lse, acc, acc_out, decay,
+                                               work));
+}
+
+int skv_cache_evict(skv_ctx* ctx, int32_t B, const float* acc, int32_t T_total, const int32_t* cu_tok, const int32_t* n_tok, int32_t max_n, int32_t keep, int32_t sink,
+                    int32_t recent, int32_t* keep_idx, int32_t* n_keep) {
+    if (!ctx) return SKV_EINVAL;
+    if (B < 1 || T_total < 1 || max_n < 0 || keep < 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > keep) return SKV_EINVAL;
+    if (bad_ptr(acc) || bad_ptr(cu_tok) || bad_ptr(n_tok) || bad_ptr(keep_idx) || bad_ptr(n_keep)) return SKV_EINVAL;
+    if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens || max_n > ctx->c.d.max_tokens) return SKV_ECAPACITY;
+    const int rc = check_ctx(ctx);
+    if (rc != SKV_OK) return rc;
+    return hip_status(skv::launch_cache_evict(&ctx->c, B, acc, T_total, cu_tok, n_tok, max_n, keep, sink, recent, keep_idx, n_keep));
+}
+
+int skv_cache_compact(skv_ctx* ctx, int32_t B, const void* K, const void* V, const float* k_scale, const float* v_scale, const float* acc, int32_t T_total, int32_t block,
+                      const int32_t* cu_tok, const int32_t* keep_idx, int32_t keep, const int32_t* n_keep, void* K_out, void* V_out, float* k_scale_out, float* v_scale_out,
+                      float* acc_out) {
+    if (!ctx) return SKV_EINVAL;
+    if (B < 1 || T_total < 1 || keep < 0 || !cache_block(block)) return SKV_EINVAL;
+    if (bad_ptr(K) || bad_ptr(V) || bad_ptr(k_scale) || bad_ptr(v_scale) || bad_ptr(cu_tok) || bad_ptr(keep_idx) || bad_ptr(n_keep) || bad_ptr(K_out) || bad_ptr(V_out) ||
+        bad_ptr(k_scale_out) || bad_ptr(v_scale_out) || !aligned16(acc) || !aligned16(acc_out) || (acc != nullptr) != (acc_out != nullptr))
+        return SKV_EINVAL;
+    const int same = (K == K_out) + (V == V_out) + (k_scale == k_scale_out) + (v_scale == v_scale_out);
+    if ((same != 0 && same != 4) || (acc && (acc == acc_out) != (same == 4))) return SKV_EINVAL;
+    if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens) return SKV_ECAPACITY;
+    const int rc = check_ctx(ctx);
+    if (rc != SKV_OK) return rc;
+    return hip_status(skv::launch_cache_compact(&ctx->c, B, K, V, k_scale, v_scale, acc, T_total, block, cu_tok, keep_idx, keep, n_keep, K_out, V_out, k_scale_out,
+                                                v_scale_out, acc_out));
 }
 
 }  // extern "C"

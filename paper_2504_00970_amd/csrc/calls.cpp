@@ -1,5 +1,5 @@
 // Calls of libsentencekv's C entry points from Python without ctypes: a pointer argument is a tensor (its data pointer) or None (a null
-// pointer), a number an integer.  Addresses as integers are taken for the context and for skv_segment's n_sent_host only, so that an
+// pointer), a number an integer, or a real number where the entry point takes a float.  Addresses as integers are taken for the context and for skv_segment's n_sent_host only, so that an
 // argument in another one's place is refused here and does not go to the GPU as an address.  ctypes and the Python code around it took 2.4 to 4.8 us per call (an is_contiguous and a
 // data_ptr call for every tensor, argument objects), more than the kernels of a short context run; this takes 0.3 to 0.7.
 // Host code only.  The entry points are looked up in the library that `load` is given, once.
@@ -50,6 +50,11 @@ bool convert(PyObject* o, T* out) {
         } else {
             return refuse(o, "a tensor or None");
         }
+    } else if constexpr (std::is_floating_point_v<T>) {
+        if (THPVariable_Check(o)) return refuse(o, "a number");
+        const double v = PyFloat_AsDouble(o);
+        if (v == -1.0 && PyErr_Occurred()) return false;
+        *out = static_cast<T>(v);
     } else {
         if (THPVariable_Check(o)) return refuse(o, "a number");
         const long long v = PyLong_AsLongLong(o);
@@ -101,7 +106,8 @@ struct Call<F> {
 
 #define SKV_CALLS(X)                                                                                                      \
     X(skv_segment) X(skv_build_semvec) X(skv_build_semvec_layers) X(skv_token_importance) X(skv_retain) X(skv_compact_pool) \
-    X(skv_query_update) X(skv_score) X(skv_select) X(skv_gather) X(skv_attend) X(skv_decode_step) X(skv_merge_lse)
+    X(skv_query_update) X(skv_score) X(skv_select) X(skv_gather) X(skv_attend) X(skv_decode_step) X(skv_merge_lse)        \
+    X(skv_rotary) X(skv_cache_append) X(skv_cache_attend) X(skv_cache_evict) X(skv_cache_compact)
 
 PyObject* load(PyObject*, PyObject* path) {
     const char* p = PyUnicode_AsUTF8(path);

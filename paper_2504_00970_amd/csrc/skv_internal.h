@@ -176,6 +176,21 @@ hipError_t launch_select_attend_stream(Ctx* c, const void* q, const void* K_laye
 hipError_t launch_merge_lse(Ctx* c, const float* out_a, const float* lse_a, const float* out_b, const float* lse_b,
                             int32_t n_heads, float* out, float* lse);
 
+// rotary positions and the 8-bit cache (cache.hip)
+hipError_t launch_rotary(Ctx* c, int32_t n, const void* q, const void* k, const int32_t* pos, const double* inv_freq, int32_t rot, bool interleaved,
+                         float mscale, void* q_out, void* k_out);
+hipError_t launch_cache_append(Ctx* c, int32_t layer, int32_t B, const void* k, const void* v, int32_t n_new, const int32_t* cu_new, int32_t max_new,
+                               const int32_t* cu_tok, const int32_t* n_tok, void* K, void* V, float* ks, float* vs, int32_t T_total, int32_t block, float* acc);
+int64_t cache_attend_work_bytes(const Ctx* c, int32_t B, int32_t max_n, bool weights);
+hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, const void* K, const void* V, const float* ks, const float* vs, int32_t T_total,
+                               int32_t block, const int32_t* cu_tok, const int32_t* n_tok, const int32_t* tok_idx, int32_t max_n, float* out, float* lse,
+                               const float* acc, float* acc_out, float decay, void* work);
+hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_total, const int32_t* cu_tok, const int32_t* n_tok, int32_t max_n, int32_t keep,
+                              int32_t sink, int32_t recent, int32_t* keep_idx, int32_t* n_keep);
+hipError_t launch_cache_compact(Ctx* c, int32_t B, const void* K, const void* V, const float* ks, const float* vs, const float* acc, int32_t T_total, int32_t block,
+                                const int32_t* cu_tok, const int32_t* keep_idx, int32_t keep, const int32_t* n_keep, void* K_out, void* V_out, float* ks_out,
+                                float* vs_out, float* acc_out);
+
 // A K/V row is D * EB bytes = LPR lanes of 16 bytes, so one wave-wide 128-bit load covers RPW
 // consecutive rows; each lane holds EPL elements of its row.
 template <int EB> struct Row;
