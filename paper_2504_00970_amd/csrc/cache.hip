@@ -80,82 +80,95 @@ template <int EB> __device__ __forceinline__ uint4 pack16(const float* f) {
     else return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
 }
 
-// VEC: rot is a multiple of 16.  Otherwise a lane turns one pair, element by element.
+// VEC: rot is a multiple of 16.  Otherwise a lane turns one pair, element by element.  A wave's table of cosines and sines is its own: no barrier.
 template <int EB, bool INTERLEAVED, bool VEC>
 __global__ __launch_bounds__(kRotWaves * kWave) void rotary_kernel(RotArgs a) {
-    __shared__ float2 table[kRotWaves][kHeadDim / 2];
+    __shared__ __align__(16) float2 table[kRotWaves][kHeadDim / 2];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t tok = (int64_t)blockIdx.x * kRotWaves + w;
-    const bool live = tok < a.n;
-    if (live && lane < a.half) {
-        const double turns = (double)a.pos[tok] * a.inv_freq[lane] * 0.15915494309189533577;
-        const float r = (float)(turns - rint(turns));
-        float s, c;
-        sincospif(2.0f * r, &s, &c);
-        table[w][lane] = make_float2(c * a.mscale, s * a.mscale);
-    }
-    __syncthreads();
-    if (!live) return;
     const int heads = a.n_q + a.n_k, h0 = blockIdx.y * a.heads_per_wave, h1 = min(heads, h0 + a.heads_per_wave);
     const int64_t row_bytes = kHeadDim * EB;
-    auto row_in = [&](int h) { return h < a.n_q ? a.q + (tok * a.n_q + h) * row_bytes : a.k + (tok * a.n_k + (h - a.n_q)) * row_bytes; };
-    auto row_out = [&](int h) { return h < a.n_q ? a.q_out + (tok * a.n_q + h) * row_bytes : a.k_out + (tok * a.n_k + (h - a.n_q)) * row_bytes; };
-    if constexpr (VEC) {
-        constexpr int E = 16 / EB, UNITS = kHeadDim / (2 * E), ROWS = kWave / UNITS;
-        const int u = lane % UNITS, n_pairs = a.half / E;
-        const bool turn = u < n_pairs;
-        const int pa = (INTERLEAVED ? 2 * u : turn ? u : 2 * u) * 16, pb = INTERLEAVED || !turn ? pa + 16 : pa + n_pairs * 16;
-        float c[E], s[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float2 t = turn ? table[w][u * E + i] : make_float2(1.0f, 0.0f);
-            c[i] = t.x;
-            s[i] = t.y;
-        }
-        for (int h = h0 + lane / UNITS; h < h1; h += ROWS) {
-            const char* in = row_in(h);
-            char* out = row_out(h);
-            uint4 va = *reinterpret_cast<const uint4*>(in + pa), vb = *reinterpret_cast<const uint4*>(in + pb);
-            if (turn) {
-                float x[2 * E], y[2 * E];
-                unpack16<EB>(va, x);
-                unpack16<EB>(vb, x + E);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const int ia = INTERLEAVED ? 2 * i : i, ib = INTERLEAVED ? 2 * i + 1 : E + i;
-                    y[ia] = x[ia] * c[i] - x[ib] * s[i];
-                    y[ib] = x[ib] * c[i] + x[ia] * s[i];
-                }
-                va = pack16<EB>(y);
-                vb = pack16<EB>(y + E);
+    for (int64_t tok = (int64_t)blockIdx.x * kRotWaves + w; tok < a.n; tok += (int64_t)gridDim.x * kRotWaves) {
+        auto row_in = [&](int h) { return h < a.n_q ? a.q + (tok * a.n_q + h) * row_bytes : a.k + (tok * a.n_k + (h - a.n_q)) * row_bytes; };
+        auto row_out = [&](int h) { return h < a.n_q ? a.q_out + (tok * a.n_q + h) * row_bytes : a.k_out + (tok * a.n_k + (h - a.n_q)) * row_bytes; };
+        auto angles = [&] {
+            if (lane < a.half) {
+                const double turns = (double)a.pos[tok] * a.inv_freq[lane] * 0.15915494309189533577;
+                const float r = (float)(turns - rint(turns));
+                float s, c;
+                sincospif(2.0f * r, &s, &c);
+                table[w][lane] = make_float2(c * a.mscale, s * a.mscale);
             }
-            *reinterpret_cast<uint4*>(out + pa) = va;
-            *reinterpret_cast<uint4*>(out + pb) = vb;
-        }
-    } else {
-        const bool turn = lane < a.half;
-        const int ea = turn && !INTERLEAVED ? lane : 2 * lane, eb = turn && !INTERLEAVED ? lane + a.half : 2 * lane + 1;
-        const float2 t = turn ? table[w][lane] : make_float2(1.0f, 0.0f);
-        for (int h = h0; h < h1; ++h) {
-            const char* in = row_in(h);
-            char* out = row_out(h);
-            if constexpr (EB == 2) {
-                const uint16_t *i16 = reinterpret_cast<const uint16_t*>(in);
-                uint16_t* o16 = reinterpret_cast<uint16_t*>(out);
-                uint32_t xa = i16[ea], xb = i16[eb];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        };
+        if constexpr (VEC) {
+            constexpr int E = 16 / EB, UNITS = kHeadDim / (2 * E), ROWS = kWave / UNITS;
+            const int u = lane % UNITS, n_pairs = a.half / E;
+            const bool turn = u < n_pairs;
+            const int pa = (INTERLEAVED ? 2 * u : turn ? u : 2 * u) * 16, pb = INTERLEAVED || !turn ? pa + 16 : pa + n_pairs * 16;
+            uint4 va, vb;
+            auto load = [&](int h) {                          // past the last head: the last one again, which is not stored
+                const char* in = row_in(min(h, heads - 1));
+                va = ld_stream(in + pa);
+                vb = ld_stream(in + pb);
+            };
+            load(h0 + lane / UNITS);                          // on its way while the angles are formed
+            angles();
+            float c[E], s[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float2 t = turn ? table[w][u * E + i] : make_float2(1.0f, 0.0f);
+                c[i] = t.x;
+                s[i] = t.y;
+            }
+            for (int hb = h0; hb < h1; hb += ROWS) {
+                const int h = hb + lane / UNITS;
                 if (turn) {
-                    const float x = __uint_as_float(xa << 16), y = __uint_as_float(xb << 16);
-                    const uint32_t z = bf16_pair(x * t.x - y * t.y, y * t.x + x * t.y);
-                    xa = z & 0xffffu;
-                    xb = z >> 16;
+                    float x[2 * E], y[2 * E];
+                    unpack16<EB>(va, x);
+                    unpack16<EB>(vb, x + E);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        const int ia = INTERLEAVED ? 2 * i : i, ib = INTERLEAVED ? 2 * i + 1 : E + i;
+                        y[ia] = x[ia] * c[i] - x[ib] * s[i];
+                        y[ib] = x[ib] * c[i] + x[ia] * s[i];
+                    }
+                    va = pack16<EB>(y);
+                    vb = pack16<EB>(y + E);
                 }
-                o16[ea] = (uint16_t)xa;
-                o16[eb] = (uint16_t)xb;
-            } else {
-                const float *f = reinterpret_cast<const float*>(in), x = f[ea], y = f[eb];
-                float* o = reinterpret_cast<float*>(out);
-                o[ea] = turn ? x * t.x - y * t.y : x;
-                o[eb] = turn ? y * t.x + x * t.y : y;
+                if (h < h1) {
+                    char* out = row_out(h);
+                    st_stream(out + pa, va);
+                    st_stream(out + pb, vb);
+                }
+                if (hb + ROWS < h1) load(h + ROWS);
+            }
+        } else {
+            angles();
+            const bool turn = lane < a.half;
+            const int ea = turn && !INTERLEAVED ? lane : 2 * lane, eb = turn && !INTERLEAVED ? lane + a.half : 2 * lane + 1;
+            const float2 t = turn ? table[w][lane] : make_float2(1.0f, 0.0f);
+            for (int h = h0; h < h1; ++h) {
+                const char* in = row_in(h);
+                char* out = row_out(h);
+                if constexpr (EB == 2) {
+                    const uint16_t* i16 = reinterpret_cast<const uint16_t*>(in);
+                    uint16_t* o16 = reinterpret_cast<uint16_t*>(out);
+                    uint32_t xa = i16[ea], xb = i16[eb];
+                    if (turn) {
+                        const float x = __uint_as_float(xa << 16), y = __uint_as_float(xb << 16);
+                        const uint32_t z = bf16_pair(x * t.x - y * t.y, y * t.x + x * t.y);
+                        xa = z & 0xffffu;
+                        xb = z >> 16;
+                    }
+                    o16[ea] = (uint16_t)xa;
+                    o16[eb] = (uint16_t)xb;
+                } else {
+                    const float *f = reinterpret_cast<const float*>(in), x = f[ea], y = f[eb];
+                    float* o = reinterpret_cast<float*>(out);
+                    o[ea] = turn ? x * t.x - y * t.y : x;
+                    o[eb] = turn ? y * t.x + x * t.y : y;
+                }
             }
         }
     }
@@ -174,79 +187,80 @@ struct AppendArgs {
     uint8_t *K, *V;             // the layer's slices
     float *ks, *vs, *acc;
     const int32_t *cu_new, *cu_tok, *n_tok;
-    int32_t n_new, max_new, T_total, n_scales, shift, n_kv;
+    int32_t n_new, max_new, T_total, n_scales, n_kv;
 };
 
 template <int EB, int BLOCK>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs a) {
-    __shared__ uint32_t most[kAppendThreads / kWave];
-    constexpr int ITERS = BLOCK / kAppendRows;
-    const int pair = blockIdx.y, b = pair / a.n_kv, h = pair % a.n_kv;
+    __shared__ uint32_t most[2][kAppendThreads / kWave];
+    constexpr int ITERS = BLOCK / kAppendRows, SHIFT = BLOCK == 16 ? 4 : BLOCK == 32 ? 5 : BLOCK == 64 ? 6 : 7;
+    const int pair = blockIdx.x, b = pair / a.n_kv, h = pair % a.n_kv;
     const bool is_v = blockIdx.z != 0;
+    const int tid = threadIdx.x, col = (tid & 15) * 8, r0 = tid >> 4;
     int32_t first, rows;
     region(a.cu_tok, b, a.T_total, &first, &rows);
     const int32_t held = min(max(a.n_tok[pair], 0), rows);
     const int32_t c0 = max(a.cu_new[b], 0), c1 = min(a.cu_new[b + 1], a.n_new);
     const int32_t m = min(min(c1 > c0 ? c1 - c0 : 0, a.max_new), rows - held);
-    const int32_t t = (held >> a.shift) + blockIdx.x, base = t << a.shift;
-    const int32_t lo = max(base, held), hi = min(base + BLOCK, held + m);     // the new rows of this block
-    if (lo >= hi) return;
-    const int tid = threadIdx.x, col = (tid & 15) * 8, r0 = tid >> 4;
-    float* scale = (is_v ? a.vs : a.ks) + (int64_t)h * a.n_scales + (first >> a.shift) + b + t;
-    const bool has_old = base < held;
-    const float old = has_old ? *scale : 0.0f;
-    const char* src = is_v ? a.v : a.k;
-    uint8_t* dst = (is_v ? a.V : a.K) + ((int64_t)h * a.T_total + first + base) * kHeadDim + col;
-
-    uint4 x[ITERS * EB / 2];
-    uint32_t big = 0;
+    if (m <= 0) return;
+    const char* src = (is_v ? a.v : a.k) + (((int64_t)c0 * a.n_kv + h) * kHeadDim + col) * EB;
+    const int64_t src_row = (int64_t)a.n_kv * kHeadDim * EB;
+    float* scales = (is_v ? a.vs : a.ks) + (int64_t)h * a.n_scales + (first >> SHIFT) + b;
+    uint8_t* pool = (is_v ? a.V : a.K) + ((int64_t)h * a.T_total + first) * kHeadDim + col;
+    int buf = 0;
+    for (int32_t t = (held >> SHIFT) + blockIdx.y; t << SHIFT < held + m; t += gridDim.y, buf ^= 1) {
+        const int32_t base = t << SHIFT, lo = max(base, held), hi = min(base + BLOCK, held + m);     // the new rows of this block
+        const bool has_old = base < held;
+        const float old = has_old ? scales[t] : 0.0f;
+        uint8_t* dst = pool + (int64_t)base * kHeadDim;
+        uint4 x[ITERS * EB / 2];                              // rows that are not new: one that is, again (a load under a condition waits for those before it)
 #pragma unroll
-    for (int i = 0; i < ITERS; ++i) {
-        const int32_t row = base + r0 + i * kAppendRows;
-        const bool in = row >= lo && row < hi;
-        const char* p = src + (((int64_t)(c0 + (in ? row - held : 0)) * a.n_kv + h) * kHeadDim + col) * EB;
+        for (int i = 0; i < ITERS; ++i) {
+            const char* p = src + (min(max(base + r0 + i * kAppendRows, lo), hi - 1) - held) * src_row;
 #pragma unroll
-        for (int j = 0; j < EB / 2; ++j) x[i * (EB / 2) + j] = in ? *reinterpret_cast<const uint4*>(p + 16 * j) : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < ITERS * EB / 2; ++i) {
-        float f[16 / EB];
-        unpack16<EB>(x[i], f);
-#pragma unroll
-        for (int j = 0; j < 16 / EB; ++j) {
-            const uint32_t u = __float_as_uint(f[j]) & 0x7fffffffu;
-            big = max(big, u < kInfBits ? u : 0u);
+            for (int j = 0; j < EB / 2; ++j) x[i * (EB / 2) + j] = ld_stream(p + 16 * j);
         }
-    }
+        uint32_t big = 0;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
-    if ((tid & 63) == 0) most[tid >> 6] = big;
-    __syncthreads();
-    big = max(max(most[0], most[1]), max(most[2], most[3]));
-    const float s = fmaxf(old, scale_of(big));
-    if (has_old && s > old) {
-        const float f = old / s;
-        for (int32_t row = r0; row < held - base; row += kAppendRows) {
-            uint2* p = reinterpret_cast<uint2*>(dst + (int64_t)row * kHeadDim);
-            const uint2 w = *p;
-            *p = make_uint2(rescale(w.x, f), rescale(w.y, f));
+        for (int i = 0; i < ITERS * EB / 2; ++i) {
+            float f[16 / EB];
+            unpack16<EB>(x[i], f);
+#pragma unroll
+            for (int j = 0; j < 16 / EB; ++j) {
+                const uint32_t u = __float_as_uint(f[j]) & 0x7fffffffu;
+                big = max(big, u < kInfBits ? u : 0u);
+            }
         }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+        if ((tid & 63) == 0) most[buf][tid >> 6] = big;
+        __syncthreads();
+        big = max(max(most[buf][0], most[buf][1]), max(most[buf][2], most[buf][3]));
+        const float s = fmaxf(old, scale_of(big));
+        if (has_old && s > old) {
+            const float f = old / s;
+            for (int32_t row = r0; row < held - base; row += kAppendRows) {
+                uint2* p = reinterpret_cast<uint2*>(dst + (int64_t)row * kHeadDim);
+                const uint2 w = *p;
+                *p = make_uint2(rescale(w.x, f), rescale(w.y, f));
+            }
+        }
+        const float inv = 1.0f / s;
+#pragma unroll
+        for (int i = 0; i < ITERS; ++i) {
+            const int32_t row = base + r0 + i * kAppendRows;
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < EB / 2; ++j) unpack16<EB>(x[i * (EB / 2) + j], f + j * (16 / EB));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] *= inv;
+            const unsigned long long w = codes_of(f[0], f[1], f[2], f[3]) | (unsigned long long)codes_of(f[4], f[5], f[6], f[7]) << 32;
+            if (row >= lo && row < hi) __builtin_nontemporal_store(w, reinterpret_cast<unsigned long long*>(dst + (int64_t)(row - base) * kHeadDim));
+        }
+        if (tid == 0) scales[t] = s;
+        if (!is_v && a.acc)
+            for (int32_t row = lo + tid; row < hi; row += kAppendThreads) a.acc[(int64_t)h * a.T_total + first + row] = 0.0f;
     }
-    const float inv = 1.0f / s;
-#pragma unroll
-    for (int i = 0; i < ITERS; ++i) {
-        const int32_t row = base + r0 + i * kAppendRows;
-        if (row < lo || row >= hi) continue;
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < EB / 2; ++j) unpack16<EB>(x[i * (EB / 2) + j], f + j * (16 / EB));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] *= inv;
-        *reinterpret_cast<uint2*>(dst + (int64_t)(row - base) * kHeadDim) = make_uint2(codes_of(f[0], f[1], f[2], f[3]), codes_of(f[4], f[5], f[6], f[7]));
-    }
-    if (tid == 0) *scale = s;
-    if (!is_v && a.acc)
-        for (int32_t row = lo + tid; row < hi; row += kAppendThreads) a.acc[(int64_t)h * a.T_total + first + row] = 0.0f;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -257,23 +271,43 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
 //            16 g .. 16 g + 15 of the first and of the second half of row c.
 //   outputs  rows = 16 of the dims, contraction over 32 tokens.  The scores leave lane (c, g) with the tokens 4 g .. 4 g + 3 of two tiles for query c, which is
 //            the right operand as it lies; the lane reads 8 bytes (dims 8 c .. 8 c + 7) of these 8 rows and transposes them in registers.
-// Eight of the sixteen columns hold queries, the others the same queries again: the first eight carry the weights' leading 8 bits, the others what is left of
-// them (the next 8), at no cost, so that a weight is off by at most 2^-18 of itself.  fp32 queries are split into three bf16 pieces that add up to them
-// exactly.  Scores, maxima, sums and outputs are fp32.
+// Eight of the sixteen columns hold queries, the others the same queries again, so that two pieces of 8 bits of the weights go through one instruction; with
+// a second one for the last piece a weight keeps 24 bits.  (With two pieces results were off by 2e-6 of themselves, with three by 5e-7; the time is the same.)  fp32
+// queries are split into three pieces that add up to them exactly.  Scores, maxima, sums and outputs are fp32.
 // A wave keeps a running reference per query (moved up only where a score exceeds it by 2^8: weights are then at most 256); the waves of a block and the blocks
 // of a (sequence, head) pair are joined by their references.
 // ------------------------------------------------------------------------------------------------
-constexpr int kCacheTile = 32;
+constexpr int kCacheTile = 32, kCacheWaves = 4, kCacheStep = kCacheTile * kCacheWaves;
+constexpr int kListedChunk = 1024;     // entries of a list per block, at most
+constexpr int kJoinInside = 32;        // parts of a pair up to which the attention kernel joins them itself
+constexpr int kSharePairs = 1024;      // pairs up to which the blocks take equal shares
+constexpr int kStageTiles = 8;         // tiles whose scores a wave keeps in LDS
+
+// How the rows are dealt to blocks.  kGrid: blocks of `chunk` rows of a (sequence, head) pair.  kList: the same of its list.  kShare: the rows of all pairs in a row, in units
+// of kCacheStep, in equal shares: sequences of unlike lengths keep every compute unit busy to the end.  A block that has rows of several pairs joins its waves
+// for each of them.
+enum CacheDeal { kGrid, kList, kShare };
 
 struct CacheAttendArgs {
     const char* q;
     const uint8_t *K, *V;       // the layer's slices
     const float *ks, *vs;
     const int32_t *cu_tok, *n_tok, *tok_idx;
-    int32_t max_n, T_total, n_scales, shift, n_kv, G, chunk, splits;
-    int64_t logit_stride;
+    int32_t max_n, T_total, n_scales, shift, n_kv, G, pairs, chunk, splits;
+    int64_t logit_rows;         // rows of a pair in `logits`: [pair][tile][G][32]
+    // Partial results by slots of G heads: part [slot][G][D] sums, ml [slot][G] (reference, normaliser).  A pair's slots lie side by side: from pair * splits on, or (kShare)
+    // from block + pair on, which no two pieces share since from one piece to the next the block or the pair goes up.
     float *out, *lse, *part, *ml, *lse2, *logits;
+    int32_t* units;             // kShare: [pairs + 1] units before each pair, for the launch that joins
+    unsigned int* arrived;      // per pair, zero between launches; null: cache_join_kernel joins
 };
+
+// 8 bytes that are read once.
+__device__ __forceinline__ uint2 ld_stream8(const void* p) {
+    typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+    const u32x2_t t = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p));
+    return make_uint2(t[0], t[1]);
+}
 
 // Sixteen codes as bf16, in two operands.
 __device__ __forceinline__ void widen16(const uint4& v, bf16x8_t* a, bf16x8_t* b) {
@@ -296,39 +330,90 @@ __device__ __forceinline__ float max_groups(float x) {        // over the lanes 
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-// PIECES: bf16 pieces of a query (1: bf16 queries, 3: fp32).  LISTED: rows by tok_idx, whose chunk and scales lie in LDS.  WEIGHTS: the scores are kept for
-// the second launch.
-template <int PIECES, bool LISTED, bool WEIGHTS, int NW>
-__global__ __launch_bounds__(NW * kWave) void cache_attend_kernel(CacheAttendArgs a) {
-    extern __shared__ __align__(16) char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, c = lane & 15, g = lane >> 4, hq = c & 7;
-    const int pair = blockIdx.y, b = pair / a.n_kv, h = pair % a.n_kv, split = blockIdx.x;
-    int32_t first, rows;
-    region(a.cu_tok, b, a.T_total, &first, &rows);
-    int32_t n = min(max(a.n_tok[pair], 0), a.max_n);
-    if (!LISTED) n = min(n, rows);
-    const int32_t j0 = split * a.chunk, j1 = min(n, j0 + a.chunk);
-    const int G = a.G;
-    if (j0 >= j1 && split > 0) return;
-    const uint8_t *Kh = a.K + ((int64_t)h * a.T_total + first) * kHeadDim, *Vh = a.V + ((int64_t)h * a.T_total + first) * kHeadDim;
-    const float *ksh = a.ks + (int64_t)h * a.n_scales + (first >> a.shift) + b, *vsh = a.vs + (int64_t)h * a.n_scales + (first >> a.shift) + b;
+// Rows in use of a pair.
+__device__ __forceinline__ int32_t rows_in_use(const CacheAttendArgs& a, int pair, bool listed, int32_t* first, int32_t* rows) {
+    region(a.cu_tok, pair / a.n_kv, a.T_total, first, rows);
+    const int32_t n = min(max(a.n_tok[pair], 0), a.max_n);
+    return listed ? n : min(n, *rows);
+}
 
-    int32_t* l_idx = reinterpret_cast<int32_t*>(smem);                // [chunk]; behind them the scales
-    float* l_ks = reinterpret_cast<float*>(smem) + a.chunk;
-    float* l_vs = l_ks + a.chunk;
-    if (LISTED) {
-        const int32_t* idx = a.tok_idx + (int64_t)pair * a.max_n;
-        for (int32_t j = tid; j < a.chunk; j += NW * kWave) {
-            int32_t row = j0 + j < j1 ? idx[j0 + j] : -1;
-            if (row < 0 || row >= rows) row = -1;
-            l_idx[j] = row;
-            l_ks[j] = row >= 0 ? ksh[row >> a.shift] : 0.0f;
-            l_vs[j] = row >= 0 ? vsh[row >> a.shift] : 0.0f;
+__device__ __forceinline__ void store_out(const CacheAttendArgs& a, int64_t qi, int d, float sum, float z, float top0) {
+    a.out[qi * kHeadDim + d] = z == 0.0f ? 0.0f : sum / z;
+    if (d == 0) {
+        const float l2 = z == 0.0f ? -__builtin_inff() : top0 + __builtin_log2f(z);
+        if (a.lse) a.lse[qi] = l2 * 0.6931471805599453f;
+        if (a.lse2) a.lse2[qi] = l2;
+    }
+}
+
+// PIECES: bf16 pieces of a query (1: bf16 queries, 3: fp32).  kList: the chunk's rows and their scales lie in LDS.  WEIGHTS: the scores are kept for the last launch.
+template <int PIECES, int DEAL, bool WEIGHTS>
+__global__ __launch_bounds__(kCacheWaves * kWave, PIECES == 1 && DEAL != kShare && !WEIGHTS ? 4 : 3) void cache_attend_kernel(CacheAttendArgs a) {
+    extern __shared__ __align__(16) char smem_all[];
+    constexpr bool LISTED = DEAL == kList;
+    constexpr int kThreads = kCacheWaves * kWave;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4, hq = c & 7;
+    const int G = a.G;
+    int32_t* s_units = reinterpret_cast<int32_t*>(smem_all);          // kShare: [pairs + 1], ahead of the rest
+    char* smem = smem_all + (DEAL == kShare ? (a.pairs + 4) / 4 * 16 : 0);
+    int pair = blockIdx.y, slot = blockIdx.y * a.splits + blockIdx.x;
+    int32_t unit = 0, unit_end = 0;
+    if (DEAL == kShare) {
+        __shared__ int32_t s_wave[kCacheWaves];
+        constexpr int kEach = kSharePairs / kThreads;
+        int32_t u[kEach], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int p = tid * kEach + i;
+            int32_t f, r;
+            u[i] = p < a.pairs ? (rows_in_use(a, p, false, &f, &r) + kCacheStep - 1) / kCacheStep : 0;
+            sum += u[i];
+        }
+        const int32_t upto = (int32_t)wave_scan_u32((uint32_t)sum);
+        if (lane == 63) s_wave[w] = upto;
+        __syncthreads();
+        int32_t before = upto - sum;
+        for (int i = 0; i < w; ++i) before += s_wave[i];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int p = tid * kEach + i;
+            if (p <= a.pairs) {
+                s_units[p] = before;
+                if (blockIdx.x == 0) a.units[p] = before;
+            }
+            before += u[i];
         }
         __syncthreads();
+        const int32_t all = s_units[a.pairs], n_blocks = min((int32_t)gridDim.x, all);
+        if ((int32_t)blockIdx.x >= n_blocks) return;
+        unit = (int32_t)((int64_t)all * blockIdx.x / n_blocks);
+        unit_end = (int32_t)((int64_t)all * (blockIdx.x + 1) / n_blocks);
+        int lo = 0, hi = a.pairs;                             // the last pair that begins at or before `unit`, of those that begin there the one with rows
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_units[mid] <= unit) lo = mid;
+            else hi = mid;
+        }
+        pair = __builtin_amdgcn_readfirstlane(lo);
+        unit = __builtin_amdgcn_readfirstlane(unit);
+        unit_end = __builtin_amdgcn_readfirstlane(unit_end);
     }
 
-    // the queries: columns c and c + 8 hold query c & 7 (zeros beyond G)
+    for (;;) {                                                // kShare: the pieces of the block's share; otherwise once
+    const int b = pair / a.n_kv, h = pair % a.n_kv;
+    const int32_t begin = DEAL == kShare ? __builtin_amdgcn_readfirstlane(s_units[pair]) : 0, stop = DEAL == kShare ? min(unit_end, (int32_t)__builtin_amdgcn_readfirstlane(s_units[pair + 1])) : 0;
+    const int32_t j0 = DEAL == kShare ? (unit - begin) * kCacheStep : (int32_t)blockIdx.x * a.chunk;
+    if (DEAL == kShare) slot = blockIdx.x + pair;
+
+    // a list's entries are asked for first: rows and scales wait for them
+    constexpr int kEntries = LISTED ? kListedChunk / kThreads : 1;
+    int32_t entry[kEntries];
+    if (LISTED) {
+        const int32_t* idx = a.tok_idx + (int64_t)pair * a.max_n;
+#pragma unroll
+        for (int i = 0; i < kEntries; ++i) entry[i] = idx[min(j0 + tid + i * kThreads, a.max_n - 1)];
+    }
+    // the queries: columns c and c + 8 hold query c & 7 (the last one again beyond G)
     bf16x8_t qf[PIECES][4];
     {
         const int64_t qrow = ((int64_t)pair * G + min(hq, G - 1)) * kHeadDim;
@@ -352,6 +437,32 @@ __global__ __launch_bounds__(NW * kWave) void cache_attend_kernel(CacheAttendArg
             }
         }
     }
+    int32_t first, rows;
+    const int32_t n = rows_in_use(a, pair, LISTED, &first, &rows);
+    const int32_t j1 = DEAL == kShare ? min(n, (stop - begin) * kCacheStep) : min(n, j0 + a.chunk), count = j1 > j0 ? j1 - j0 : 0;       // entries of this piece
+    if (DEAL != kShare && count == 0 && blockIdx.x > 0) return;
+    // rows: the piece's first row, with 32-bit offsets from it; a list: the sequence's first row
+    const int64_t row0 = (int64_t)h * a.T_total + first + (LISTED ? 0 : j0);
+    const uint8_t *Kh = a.K + row0 * kHeadDim, *Vh = a.V + row0 * kHeadDim;
+    const float *ksh = a.ks + (int64_t)h * a.n_scales + (first >> a.shift) + b, *vsh = a.vs + (int64_t)h * a.n_scales + (first >> a.shift) + b;
+
+    int32_t* l_idx = reinterpret_cast<int32_t*>(smem);                // [chunk]; behind them the scales
+    float* l_ks = reinterpret_cast<float*>(smem) + a.chunk;
+    float* l_vs = l_ks + a.chunk;
+    // WEIGHTS: the wave's scores of up to kStageTiles tiles, [tile][G][32].  A store to memory for every tile would be waited for with the next tile's loads.
+    float* l_x = reinterpret_cast<float*>(smem) + w * G * kStageTiles * kCacheTile;
+    float e_ks[kEntries], e_vs[kEntries];
+    if (LISTED) {
+#pragma unroll
+        for (int i = 0; i < kEntries; ++i) {
+            const int32_t j = tid + i * kThreads;
+            if (j >= count || entry[i] < 0 || entry[i] >= rows) entry[i] = -1;
+            if (j < a.chunk) l_idx[j] = entry[i];
+            e_ks[i] = ksh[max(entry[i], 0) >> a.shift];
+            e_vs[i] = vsh[max(entry[i], 0) >> a.shift];
+        }
+        __syncthreads();
+    }
 
     constexpr float kToLog2 = 0.08838834764831844f * 1.4426950408889634f;      // 1 / sqrt(D), base 2
     const float neg_inf = -__builtin_inff();
@@ -359,59 +470,117 @@ __global__ __launch_bounds__(NW * kWave) void cache_attend_kernel(CacheAttendArg
     f32x4_t o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    uint4 kt[4];                                              // the tile's codes: K, then V
+    uint2 vv[8];
+    float sk[2], sv2[2];                                      // rows: the scales of the tile's two groups of 16 (blocks are multiples of 16)
 
-    struct Tile { uint4 k[4]; uint2 v[8]; };
-    auto row_of = [&](int32_t j) -> int32_t {                 // a row of the pool to read for entry j of the chunk
-        if (LISTED) return max(l_idx[j], 0);
-        return min(j0 + j, j1 - 1);
-    };
-    auto load = [&](Tile& t, int32_t j /* first entry of the tile, in the chunk */) {
+    // A tile's scales are asked for with its keys: loads return in order, so that scales asked for later would be waited for with everything before them.
+    auto load_k = [&](int32_t j /* first entry of the tile, in the piece */) {
+        if (LISTED) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint8_t* p = Kh + (int64_t)row_of(j + 16 * i + c) * kHeadDim + 16 * g;
-            t.k[2 * i] = *reinterpret_cast<const uint4*>(p);
-            t.k[2 * i + 1] = *reinterpret_cast<const uint4*>(p + 64);
+            for (int i = 0; i < 2; ++i) {
+                const uint8_t* p = Kh + (int64_t)max(l_idx[min(j + 16 * i + c, a.chunk - 1)], 0) * kHeadDim + 16 * g;
+                kt[2 * i] = ld_stream(p);
+                kt[2 * i + 1] = ld_stream(p + 64);
+            }
+            return;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            t.v[i] = *reinterpret_cast<const uint2*>(Vh + (int64_t)row_of(j + 16 * (i >> 2) + 4 * g + (i & 3)) * kHeadDim + 8 * c);
+        for (int i = 0; i < 2; ++i) {
+            const int32_t blk = min(j0 + j + 16 * i, j1 - 1) >> a.shift;
+            sk[i] = ksh[blk];
+            sv2[i] = vsh[blk];
+        }
+        const uint8_t* base = Kh + (uint32_t)j * kHeadDim;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t off = (uint32_t)min(16 * i + c, count - 1 - j) * kHeadDim + 16 * g;
+            kt[2 * i] = *reinterpret_cast<const uint4*>(base + off);          // halves of a line: a non-temporal load of one may lose the other
+            kt[2 * i + 1] = *reinterpret_cast<const uint4*>(base + off + 64);
+        }
     };
-    auto use = [&](Tile& t, int32_t j) {
+    auto load_v = [&](int32_t j) {
+        const uint8_t* base = LISTED ? Vh : Vh + (uint32_t)j * kHeadDim;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = 16 * (i >> 2) + 4 * g + (i & 3);
+            if (LISTED) vv[i] = ld_stream8(base + (int64_t)max(l_idx[min(j + e, a.chunk - 1)], 0) * kHeadDim + 8 * c);
+            else vv[i] = ld_stream8(base + (uint32_t)(min(e, count - 1 - j) * kHeadDim + 8 * c));
+        }
+    };
+    // WEIGHTS: the staged tiles, the first of them at entry j, to memory
+    auto flush = [&](int32_t j) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        float* to = a.logits + ((int64_t)pair * a.logit_rows + j0 + j) * G;
+        for (int e = lane * 4; e < kStageTiles * G * kCacheTile; e += kWave * 4) {
+            const int tile = e / (G * kCacheTile);            // a power of two
+            if (j + tile * kCacheStep < count)
+                *reinterpret_cast<f32x4_t*>(to + (int64_t)tile * kCacheStep * G + (e & (G * kCacheTile - 1))) = *reinterpret_cast<const f32x4_t*>(l_x + e);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+
+    int32_t j = w * kCacheTile, staged = j;
+    if (j < count) {
+        load_k(j);
+        load_v(j);
+    }
+    if (LISTED) {                                             // the scales, while the first rows are on their way
+#pragma unroll
+        for (int i = 0; i < kEntries; ++i) {
+            const int32_t e = tid + i * kThreads;
+            if (e < a.chunk) {
+                l_ks[e] = e_ks[i] * kToLog2;
+                l_vs[e] = e_vs[i];
+            }
+        }
+        __syncthreads();
+    }
+    for (; j < count; j += kCacheStep) {
         float x[8], sv[8];
+        const bool tail = LISTED || j + kCacheTile > count;   // some of its entries may be none
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int f = 0; f < 2; ++f) {
                 bf16x8_t ka, kb;
-                widen16(t.k[2 * i + f], &ka, &kb);
+                widen16(kt[2 * i + f], &ka, &kb);
 #pragma unroll
                 for (int p = PIECES - 1; p >= 0; --p) {
                     s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[p][2 * f], s, 0, 0, 0);
                     s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb, qf[p][2 * f + 1], s, 0, 0, 0);
                 }
             }
-            if (LISTED) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int32_t e = j + 16 * i + 4 * g + r;
-                    x[4 * i + r] = l_idx[e] >= 0 ? s[r] * (l_ks[e] * kToLog2) : neg_inf;
-                    sv[4 * i + r] = l_vs[e];
-                }
-            } else {
-                const int32_t blk = min(j0 + j + 16 * i, j1 - 1) >> a.shift;       // blocks are multiples of 16 rows
-                const float sk = ksh[blk] * kToLog2, s2 = vsh[blk];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    x[4 * i + r] = j0 + j + 16 * i + 4 * g + r < j1 ? s[r] * sk : neg_inf;
-                    sv[4 * i + r] = s2;
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int32_t e = j + 16 * i + 4 * g + r;
+                x[4 * i + r] = s[r] * (LISTED ? l_ks[e] : sk[i] * kToLog2);
+                sv[4 * i + r] = LISTED ? l_vs[e] : sv2[i];
             }
         }
-        if (WEIGHTS && c < G) {
-            float* p = a.logits + ((int64_t)pair * G + c) * a.logit_stride + j0 + j + 4 * g;
-            *reinterpret_cast<f32x4_t*>(p) = f32x4_t{x[0], x[1], x[2], x[3]};
-            *reinterpret_cast<f32x4_t*>(p + 16) = f32x4_t{x[4], x[5], x[6], x[7]};
+        if (tail) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int32_t e = j + 16 * (i >> 2) + 4 * g + (i & 3);
+                if (LISTED ? l_idx[e] < 0 : e >= count) x[i] = neg_inf;
+            }
+        }
+        // The next tile's keys, while the rest of this one is computed, and its values behind the last use of these.  Past the last tile that is one row again: loads
+        // under a condition would make the compiler wait for the values where it waits for the keys.
+        const int32_t next = min(j + kCacheStep, count - 1);
+        load_k(next);
+        if (WEIGHTS) {
+            const int at = (j - staged) / kCacheStep;
+            if (c < G) {
+                float* p = l_x + (at * G + c) * kCacheTile + 4 * g;
+                *reinterpret_cast<f32x4_t*>(p) = f32x4_t{x[0], x[1], x[2], x[3]};
+                *reinterpret_cast<f32x4_t*>(p + 16) = f32x4_t{x[4], x[5], x[6], x[7]};
+            }
+            if (at == kStageTiles - 1 || j + kCacheStep >= count) {
+                flush(staged);
+                staged = j + kCacheStep;
+            }
         }
         float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
         top = max_groups(top);
@@ -424,7 +593,8 @@ __global__ __launch_bounds__(NW * kWave) void cache_attend_kernel(CacheAttendArg
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] *= f;
         }
-        bf16x8_t pf;
+        // the weights (times the rows' scales) in three pieces of 8 bits: the first columns carry the leading and the last one, the others the middle one
+        bf16x8_t pf, pl;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             x[i] = __builtin_amdgcn_exp2f(x[i] - sub);
@@ -434,57 +604,48 @@ __global__ __launch_bounds__(NW * kWave) void cache_attend_kernel(CacheAttendArg
         for (int i = 0; i < 8; i += 2) {
             const float y0 = x[i] * sv[i], y1 = x[i + 1] * sv[i + 1];
             const uint32_t lead = bf16_pair(y0, y1);
-            const uint32_t rest = bf16_pair(y0 - __uint_as_float(lead << 16), y1 - __uint_as_float(lead & 0xffff0000u));
-            const bf16x2_t pr = __builtin_bit_cast(bf16x2_t, c < 8 ? lead : rest);
-            pf[i] = pr[0];
-            pf[i + 1] = pr[1];
+            const float r0 = y0 - __uint_as_float(lead << 16), r1 = y1 - __uint_as_float(lead & 0xffff0000u);
+            const uint32_t mid = bf16_pair(r0, r1), low = bf16_pair(r0 - __uint_as_float(mid << 16), r1 - __uint_as_float(mid & 0xffff0000u));
+            const bf16x2_t a2 = __builtin_bit_cast(bf16x2_t, c < 8 ? lead : mid), b2 = __builtin_bit_cast(bf16x2_t, c < 8 ? low : 0u);
+            pf[i] = a2[0];
+            pf[i + 1] = a2[1];
+            pl[i] = b2[0];
+            pl[i + 1] = b2[1];
         }
-        if (LISTED || j0 + j + kCacheTile > j1) {             // what is masked may be NaN, which no weight of zero takes away
+        if (tail) {                                           // what is masked may be NaN, which no weight of zero takes away
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int32_t e = j + 16 * (i >> 2) + 4 * g + (i & 3);
-                if (LISTED ? l_idx[e] < 0 : j0 + e >= j1) t.v[i] = make_uint2(0, 0);
+                if (LISTED ? l_idx[e] < 0 : e >= count) vv[i] = make_uint2(0, 0);
             }
         }
-        bf16x8_t vt[8];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
+        for (int d = 0; d < 4; ++d) {                         // dims 2 d and 2 d + 1 of the lane's 8 rows
+            bf16x8_t va, vb;
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {                     // dims 2 d and 2 d + 1 of tokens i and i + 1
-                const uint32_t lo = d < 2 ? t.v[i].x : t.v[i].y, hi = d < 2 ? t.v[i + 1].x : t.v[i + 1].y;
+            for (int i = 0; i < 8; i += 2) {
+                const uint32_t lo = d < 2 ? vv[i].x : vv[i].y, hi = d < 2 ? vv[i + 1].x : vv[i + 1].y;
                 const uint32_t m = __builtin_amdgcn_perm(hi, lo, d & 1 ? 0x07030602u : 0x05010400u);
                 const bf16x2_t e0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(m, 1.0f, false), e1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(m, 1.0f, true);
-                vt[2 * d][i] = e0[0];
-                vt[2 * d][i + 1] = e0[1];
-                vt[2 * d + 1][i] = e1[0];
-                vt[2 * d + 1][i + 1] = e1[1];
+                va[i] = e0[0];
+                va[i + 1] = e0[1];
+                vb[i] = e1[0];
+                vb[i + 1] = e1[1];
             }
+            o[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl, o[2 * d], 0, 0, 0);
+            o[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pl, o[2 * d + 1], 0, 0, 0);
+            o[2 * d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pf, o[2 * d], 0, 0, 0);
+            o[2 * d + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, pf, o[2 * d + 1], 0, 0, 0);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[i], pf, o[i], 0, 0, 0);
-    };
-
-    const int32_t count = j1 > j0 ? j1 - j0 : 0;
-    Tile t0, t1;
-    int32_t j = w * kCacheTile;
-    constexpr int kStep = NW * kCacheTile;
-    if (j < count) load(t0, j);
-    while (j < count) {
-        if (j + kStep < count) load(t1, j + kStep);
-        use(t0, j);
-        j += kStep;
-        if (j >= count) break;
-        if (j + kStep < count) load(t0, j + kStep);
-        use(t1, j);
-        j += kStep;
+        load_v(next);
     }
 
     // join the waves: both halves of the columns, then all waves by their references
     l = sum_halves(sum_rows16(l));
-    float* s_ref = reinterpret_cast<float*>(smem);            // [NW][8], then [NW][8] sums, then [NW][8][D]
-    float* s_l = s_ref + NW * 8;
-    float* s_o = s_l + NW * 8;
-    if (LISTED) __syncthreads();
+    float* s_ref = reinterpret_cast<float*>(smem);            // [waves][8], then [waves][8] sums, then [waves][8][D]
+    float* s_l = s_ref + kCacheWaves * 8;
+    float* s_o = s_l + kCacheWaves * 8;
+    if (LISTED || WEIGHTS) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -501,85 +662,170 @@ __global__ __launch_bounds__(NW * kWave) void cache_attend_kernel(CacheAttendArg
                 *reinterpret_cast<f32x4_t*>(s_o + ((w * 8 + c) * kHeadDim + (4 * g + r) * 8 + i)) = f32x4_t{o[i][r], o[i + 1][r], o[i + 2][r], o[i + 3][r]};
     }
     __syncthreads();
-    for (int e = tid; e < G * kHeadDim; e += NW * kWave) {
+    for (int e = tid; e < G * kHeadDim; e += kThreads) {
         const int qg = e / kHeadDim, d = e % kHeadDim;
         float top = neg_inf;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) top = fmaxf(top, s_ref[i * 8 + qg]);
+        for (int i = 0; i < kCacheWaves; ++i) top = fmaxf(top, s_ref[i * 8 + qg]);
         const float top0 = top == neg_inf ? 0.0f : top;
         float sum = 0.0f, z = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
+        for (int i = 0; i < kCacheWaves; ++i) {
             const float f = __builtin_amdgcn_exp2f(s_ref[i * 8 + qg] - top0);
             z += f * s_l[i * 8 + qg];
             sum += f * s_o[(i * 8 + qg) * kHeadDim + d];
         }
-        const int64_t qi = (int64_t)pair * G + qg;
-        if (a.splits == 1) {
-            a.out[qi * kHeadDim + d] = z == 0.0f ? 0.0f : sum / z;
-            if (d == 0) {
-                const float l2 = z == 0.0f ? neg_inf : top0 + __builtin_log2f(z);
-                if (a.lse) a.lse[qi] = l2 * 0.6931471805599453f;
-                if (WEIGHTS) a.lse2[qi] = l2;
-            }
+        if (DEAL != kShare && a.splits == 1) {
+            store_out(a, (int64_t)pair * G + qg, d, sum, z, top0);
+            continue;
+        }
+        const int64_t pi = (int64_t)slot * G + qg;
+        if (DEAL != kShare && a.arrived) {
+            st_agent(a.part + pi * kHeadDim + d, sum);
+            if (d == 0) st_agent64(reinterpret_cast<float2*>(a.ml) + pi, top, z);
         } else {
-            const int64_t pi = qi * a.splits + split;
             a.part[pi * kHeadDim + d] = sum;
             if (d == 0) *reinterpret_cast<float2*>(a.ml + 2 * pi) = make_float2(top, z);
         }
     }
+    if (DEAL == kShare) {
+        if (stop >= unit_end) return;
+        unit = stop;
+        for (++pair; __builtin_amdgcn_readfirstlane(s_units[pair + 1]) <= unit; ++pair) {}      // `unit` belongs to a pair, since it is below the last one's end
+        __syncthreads();
+        continue;
+    }
+    if (!a.arrived) return;
+
+    // few parts: the block that arrives last joins them, head by head in a fixed order
+    __shared__ int s_last;
+    const int parts = max(1, (n + a.chunk - 1) / a.chunk);
+    block_sync_after_stores();
+    if (tid == 0) {
+        const bool last = __hip_atomic_fetch_add(a.arrived + pair, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)parts - 1;
+        if (last) st_agent(a.arrived + pair, 0u);
+        s_last = last;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    float2* s_ml = reinterpret_cast<float2*>(smem);           // [parts][G], at most 8 * kJoinInside
+    const int64_t pi0 = (int64_t)pair * a.splits * G;
+    for (int e = tid; e < G * parts; e += kThreads) {
+        const unsigned long long v = ld_agent64(a.ml + 2 * (pi0 + e));
+        s_ml[e] = make_float2(lo_f(v), hi_f(v));
+    }
+    __syncthreads();
+    for (int e = tid; e < G * (kHeadDim / 2); e += kThreads) {
+        const int qg = e / (kHeadDim / 2), d = e % (kHeadDim / 2) * 2;
+        const float* part = a.part + (pi0 + qg) * kHeadDim + d;
+        float top = neg_inf, z = 0.0f, s0 = 0.0f, s1 = 0.0f;
+        for (int i = 0; i < parts; ++i) top = fmaxf(top, s_ml[i * G + qg].x);
+        const float top0 = top == neg_inf ? 0.0f : top;
+#pragma unroll 8
+        for (int i = 0; i < parts; ++i) {
+            const unsigned long long v = ld_agent64(part + (int64_t)i * G * kHeadDim);
+            const float f = __builtin_amdgcn_exp2f(s_ml[i * G + qg].x - top0);
+            z += f * s_ml[i * G + qg].y;
+            s0 += f * lo_f(v);
+            s1 += f * hi_f(v);
+        }
+        const int64_t qi = (int64_t)pair * G + qg;
+        store_out(a, qi, d, s0, z, top0);
+        store_out(a, qi, d + 1, s1, z, top0);
+    }
+    return;
+    }
 }
 
-// Joins the partial results of the blocks of a (sequence, query head): one block of D threads each.
-__global__ __launch_bounds__(kHeadDim) void cache_join_kernel(CacheAttendArgs a, int listed) {
+// Joins the partial results of the blocks of a (sequence, query head): a block for each quarter of the dims, the normaliser first, then the sums of 32 parts at a time.
+constexpr int kJoinThreads = 256, kJoinDims = 32, kJoinRows = kJoinThreads / (kJoinDims / 4);
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheAttendArgs a, int listed, int blocks /* kShare: of the attention; 0: not so */) {
+    __shared__ float s_top[kJoinThreads / kWave], s_z[kJoinThreads / kWave];
+    __shared__ __align__(16) float s_o[kJoinRows][kJoinDims];
     const int64_t qi = blockIdx.x;
-    const int pair = (int)(qi / a.G), b = pair / a.n_kv, d = threadIdx.x;
-    int32_t first, rows;
-    region(a.cu_tok, b, a.T_total, &first, &rows);
-    int32_t n = min(max(a.n_tok[pair], 0), a.max_n);
-    if (!listed) n = min(n, rows);
-    const int splits = max(1, (n + a.chunk - 1) / a.chunk);
-    const float2* ml = reinterpret_cast<const float2*>(a.ml) + qi * a.splits;
-    const float* part = a.part + qi * a.splits * kHeadDim + d;
+    const int pair = (int)(qi / a.G), qg = (int)(qi % a.G), tid = threadIdx.x, r = tid / (kJoinDims / 4), d = tid % (kJoinDims / 4) * 4;
+    int splits;
+    int64_t slot;
+    if (blocks) {
+        // a pair's first and last block: of n blocks, block k takes the units from floor(all k / n) on
+        const int64_t all = a.units[a.pairs], u0 = a.units[pair], u1 = a.units[pair + 1], nb = min((int64_t)blocks, all);
+        const int64_t k0 = u1 > u0 ? ((u0 + 1) * nb + all - 1) / all - 1 : 0, k1 = u1 > u0 ? (u1 * nb + all - 1) / all - 1 : -1;
+        splits = (int)(k1 - k0 + 1);
+        slot = k0 + pair;
+    } else {
+        int32_t first, rows;
+        splits = max(1, (rows_in_use(a, pair, listed != 0, &first, &rows) + a.chunk - 1) / a.chunk);
+        slot = (int64_t)pair * a.splits;
+    }
+    const float2* ml = reinterpret_cast<const float2*>(a.ml) + slot * a.G + qg;
+    const float* part = a.part + (slot * a.G + qg) * kHeadDim + blockIdx.y * kJoinDims + d;
     const float neg_inf = -__builtin_inff();
     float top = neg_inf;
-    for (int i = 0; i < splits; ++i) top = fmaxf(top, ml[i].x);
+    for (int i = tid; i < splits; i += kJoinThreads) top = fmaxf(top, ml[(int64_t)i * a.G].x);
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    if ((tid & 63) == 0) s_top[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
     const float top0 = top == neg_inf ? 0.0f : top;
-    float sum = 0.0f, z = 0.0f;
-    for (int i = 0; i < splits; ++i) {
-        const float f = __builtin_amdgcn_exp2f(ml[i].x - top0);
-        z += f * ml[i].y;
-        sum += f * part[(int64_t)i * kHeadDim];
+    float z = 0.0f;
+    for (int i = tid; i < splits; i += kJoinThreads) {
+        const float2 v = ml[(int64_t)i * a.G];
+        z += __builtin_amdgcn_exp2f(v.x - top0) * v.y;
     }
-    a.out[qi * kHeadDim + d] = z == 0.0f ? 0.0f : sum / z;
-    if (d == 0) {
-        const float l2 = z == 0.0f ? neg_inf : top0 + __builtin_log2f(z);
-        if (a.lse) a.lse[qi] = l2 * 0.6931471805599453f;
-        if (a.lse2) a.lse2[qi] = l2;
+    for (int m = 32; m; m >>= 1) z += __shfl_xor(z, m);
+    if ((tid & 63) == 0) s_z[tid >> 6] = z;
+    __syncthreads();
+    z = (s_z[0] + s_z[1]) + (s_z[2] + s_z[3]);
+    f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int i = r; i < splits; i += kJoinRows) sum += __builtin_amdgcn_exp2f(ml[(int64_t)i * a.G].x - top0) * *reinterpret_cast<const f32x4_t*>(part + (int64_t)i * a.G * kHeadDim);
+    *reinterpret_cast<f32x4_t*>(&s_o[r][d]) = sum;
+    __syncthreads();
+    if (tid < kJoinDims) {
+        float v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kJoinRows; ++i) v += s_o[i][tid];
+        store_out(a, qi, blockIdx.y * kJoinDims + tid, v, z, top0);
     }
 }
 
 // acc_out = decay * acc + the weights of the head's G queries, from the scores and the normalisers of the launches before.
-constexpr int kWeightThreads = 256;
+constexpr int kWeightThreads = 256, kWeightRows = 4;      // rows a thread
+template <int G>
 __global__ __launch_bounds__(kWeightThreads) void cache_weights_kernel(CacheAttendArgs a, const float* acc, float* acc_out, float decay) {
     const int pair = blockIdx.y, b = pair / a.n_kv, h = pair % a.n_kv;
     int32_t first, rows;
     region(a.cu_tok, b, a.T_total, &first, &rows);
     const int32_t n = min(min(max(a.n_tok[pair], 0), a.max_n), rows);
-    const int32_t j = blockIdx.x * kWeightThreads + threadIdx.x;
+    const int32_t j = (blockIdx.x * kWeightThreads + threadIdx.x) * kWeightRows;
     if (j >= n) return;
     const int64_t at = (int64_t)h * a.T_total + first + j;
-    float sum = acc ? decay * acc[at] : 0.0f;
-    for (int g = 0; g < a.G; ++g) {
-        const float l2 = a.lse2[(int64_t)pair * a.G + g], x = a.logits[((int64_t)pair * a.G + g) * a.logit_stride + j];
-        sum += l2 == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x - l2);
+    f32x4_t x[G];                                             // scores of 4 rows: 16-byte loads; the weights begin anywhere
+    float l2[G], old[kWeightRows], sum[kWeightRows];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        x[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(a.logits + ((int64_t)pair * a.logit_rows + j / kCacheTile * kCacheTile) * G + g * kCacheTile + j % kCacheTile));
+        l2[g] = a.lse2[(int64_t)pair * G + g];
     }
-    acc_out[at] = sum;
+#pragma unroll
+    for (int r = 0; r < kWeightRows; ++r) old[r] = acc && j + r < n ? acc[at + r] : 0.0f;
+#pragma unroll
+    for (int r = 0; r < kWeightRows; ++r) sum[r] = acc ? decay * old[r] : 0.0f;
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int r = 0; r < kWeightRows; ++r) sum[r] += l2[g] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x[g][r] - l2[g]);
+#pragma unroll
+    for (int r = 0; r < kWeightRows; ++r)
+        if (j + r < n) acc_out[at + r] = sum[r];
 }
 
 // ------------------------------------------------------------------------------------------------
-// Eviction: which rows of a (layer, sequence, head) stay.  One block each.  The cut is found digit by digit (11, 11, 10 bits) in the order-preserving images of the
-// weights, the kept rows are then written in order: every wave counts what it keeps of its share, and writes it behind the shares before.
+// Eviction: which rows of a (layer, sequence, head) stay.  One block each: every wave takes a share of neighbouring rows.  The cut is found digit by digit (11, 11, 10 bits) in
+// the order-preserving images of the weights; every wave then counts what it keeps of its share and writes it behind the shares before, in order.
+// KEYS: up to KEYS * 1024 rows, whose images stay in registers: the weights are read once.  0: any number, read in each of the five passes.
+// Counters: four of each digit, taken by lane, since gathered weights crowd into few digits (half of the rows may have the same one) and lanes that
+// add to one counter queue for it.
 // ------------------------------------------------------------------------------------------------
 struct EvictArgs {
     const float* acc;
@@ -587,9 +833,11 @@ struct EvictArgs {
     int32_t B, n_kv, T_total, max_n, keep, sink, recent;
     int32_t *keep_idx, *n_keep;
 };
+constexpr int kEvictDigits = 2048, kEvictCopies = 4;
 
+template <int KEYS>
 __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a) {
-    __shared__ uint32_t hist[2048];
+    __shared__ __align__(16) uint32_t hist[kEvictDigits * kEvictCopies];
     __shared__ uint32_t slot[kBlockWaves], slot2[kBlockWaves], found[2];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t row = blockIdx.x;                            // (layer * B + b) * Hkv + h
@@ -604,79 +852,133 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
         for (int32_t j = tid; j < n; j += kBlockThreads) out[j] = j;
         return;
     }
+    if (a.keep == 0) return;
     const float* acc = a.acc + (layer * a.n_kv + h) * (int64_t)a.T_total + first;
-    const int32_t lo = a.sink, hi = n - a.recent;              // the rows that compete
-    uint32_t need = (uint32_t)(a.keep - a.sink - a.recent);    // of them stay
-    uint32_t prefix = 0, mask = 0;
-    if (need > 0) {
-#pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-            for (int i = tid; i < 2048; i += kBlockThreads) hist[i] = 0;
-            __syncthreads();
-            for (int32_t j = lo + tid; j < hi; j += kBlockThreads) {
-                const uint32_t key = score_key(acc[j]);
-                if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1u);
-            }
-            __syncthreads();
-            // digits from the largest down, two a thread: the one in which the count reaches `need`
-            const uint32_t d0 = 2047 - 2 * tid, c0 = hist[d0], c1 = hist[d0 - 1];
-            uint32_t total;
-            const uint32_t upto = block_scan_u32(c0 + c1, slot, &total), before = upto - c0 - c1;
-            if (before < need && need <= upto) {
-                const bool second = need > before + c0;
-                found[0] = d0 - (second ? 1 : 0);
-                found[1] = need - before - (second ? c0 : 0);
-            }
-            __syncthreads();
-            prefix |= found[0] << shift;
-            mask |= ((1u << bits) - 1) << shift;
-            need = found[1];
-        }
-    }
-    // every row whose key is above `prefix`, and the first `need` of those equal to it; with need == 0 no row that competes
-    const bool any = a.keep > a.sink + a.recent;
     const int32_t share = (n + kBlockThreads - 1) / kBlockThreads * 64, s0 = min(n, w * share), s1 = min(n, s0 + share);
-    uint32_t above = 0, equal = 0;
-    auto look = [&](int32_t j, bool* gt, bool* eq) {
-        const bool in = j < s1, safe = j < lo || j >= hi;
-        const uint32_t key = in && !safe ? score_key(acc[j]) : 0u;
-        *gt = in && (safe || (any && key > prefix));
-        *eq = in && !safe && any && key == prefix;
+    const int copy = lane & (kEvictCopies - 1);
+    // the images: rows that stay whatever they weigh above all others, lanes without a row below them (with NaN, which `in` tells apart)
+    auto image = [&](int32_t j0 /* of the wave's first lane */, float f) -> uint32_t {
+        uint32_t key = score_key(f);
+        if (j0 < a.sink || j0 + 64 > min(n - a.recent, s1)) {
+            const int32_t j = j0 + lane;
+            key = j >= s1 ? 0u : j < a.sink || j >= n - a.recent ? 0xffffffffu : key;
+        }
+        return key;
     };
-    for (int32_t j = s0 + lane; j - lane < s1; j += 64) {
-        bool gt, eq;
-        look(j, &gt, &eq);
-        above += (uint32_t)__popcll(__ballot(gt));
-        equal += (uint32_t)__popcll(__ballot(eq));
+    uint32_t keys[KEYS ? KEYS : 1];
+    if constexpr (KEYS > 0) {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) keys[i] = __float_as_uint(acc[min(s0 + i * 64 + lane, n - 1)]);   // a load under a condition would wait for the one before
+    }
+    for (int i = tid; i < kEvictDigits; i += kBlockThreads) *reinterpret_cast<uint4*>(hist + 4 * i) = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    // f(i, first row, the lane's image) for the wave's rows, 64 at a time
+    auto each = [&](auto f) {
+        if constexpr (KEYS > 0) {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i)
+                if (s0 + i * 64 < s1) f(i, s0 + i * 64, keys[i]);
+        } else {
+            for (int32_t j0 = s0; j0 < s1; j0 += 64) f(0, j0, image(j0, acc[min(j0 + lane, n - 1)]));
+        }
+    };
+    uint32_t need = (uint32_t)a.keep, prefix = 0;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t digits = pass == 2 ? 1024u : 2048u;
+        each([&](int i, int32_t j0, uint32_t key) {
+            if (KEYS > 0 && pass == 0) keys[i] = key = image(j0, __uint_as_float(key));
+            if (pass == 0 || (key >> (pass == 1 ? 21 : 10)) == prefix) atomicAdd(&hist[((key >> shift) & (digits - 1)) * kEvictCopies + copy], 1u);
+        });
+        __syncthreads();
+        // digits from the largest down, two a thread: the one in which the count reaches `need`
+        const uint32_t d0 = 2047 - 2 * tid;
+        uint4 *p0 = reinterpret_cast<uint4*>(hist + d0 * 4), *p1 = reinterpret_cast<uint4*>(hist + (d0 - 1) * 4);
+        const uint4 h0 = *p0, h1 = *p1;
+        *p0 = make_uint4(0, 0, 0, 0);                         // for the next pass
+        *p1 = make_uint4(0, 0, 0, 0);
+        const uint32_t c0 = h0.x + h0.y + h0.z + h0.w, c1 = h1.x + h1.y + h1.z + h1.w;
+        uint32_t total;
+        const uint32_t upto = block_scan_u32(c0 + c1, slot, &total), before = upto - c0 - c1;
+        if (before < need && need <= upto) {
+            const bool second = need > before + c0;
+            found[0] = d0 - (second ? 1 : 0);
+            found[1] = need - before - (second ? c0 : 0);
+        }
+        __syncthreads();
+        prefix = (prefix << (pass == 2 ? 10 : 11)) | found[0];
+        need = found[1];
+    }
+    // every row whose image is above `prefix`, and the first `need` of those equal to it.  A lane's kept rows are bits of a word where its images are in registers.
+    uint32_t above = 0, equal = 0, kept_rows = 0, equal_rows = 0;
+    each([&](int i, int32_t j0, uint32_t key) {
+        if constexpr (KEYS > 0) {
+            kept_rows |= key > prefix ? 1u << i : 0u;
+            equal_rows |= key == prefix ? 1u << i : 0u;
+        } else {
+            above += (uint32_t)__popcll(__ballot(key > prefix));
+            equal += (uint32_t)__popcll(__ballot(key == prefix && j0 + lane < s1));
+        }
+    });
+    if constexpr (KEYS > 0) {
+        if (prefix == 0) equal_rows &= s0 + lane < s1 ? (2u << ((s1 - 1 - s0 - lane) >> 6)) - 1 : 0u;      // NaN: lanes without a row look the same
+        above = __builtin_amdgcn_readlane((int)wave_scan_u32((uint32_t)__popc(kept_rows)), 63);
+        equal = __builtin_amdgcn_readlane((int)wave_scan_u32((uint32_t)__popc(equal_rows)), 63);
     }
     if (lane == 0) {
         slot[w] = above;
         slot2[w] = equal;
     }
     __syncthreads();
-    uint32_t gt_before = 0, eq_before = 0;
-    for (int i = 0; i < w; ++i) {
-        gt_before += slot[i];
-        eq_before += slot2[i];
+    uint32_t before = lane < w ? slot[lane] : 0u, eq_before = lane < w ? slot2[lane] : 0u;
+#pragma unroll
+    for (int m = 1; m < kBlockWaves; m <<= 1) {
+        before += (uint32_t)__shfl_xor((int)before, m);
+        eq_before += (uint32_t)__shfl_xor((int)eq_before, m);
     }
-    const unsigned long long below = (1ull << lane) - 1;
-    for (int32_t j = s0 + lane; j - lane < s1; j += 64) {
-        bool gt, eq;
-        look(j, &gt, &eq);
-        const unsigned long long bg = __ballot(gt), be = __ballot(eq);
-        const uint32_t g_at = gt_before + (uint32_t)__popcll(bg & below), e_at = eq_before + (uint32_t)__popcll(be & below);
-        if (gt || (eq && e_at < need)) out[g_at + min(e_at, need)] = j;
-        gt_before += (uint32_t)__popcll(bg);
-        eq_before += (uint32_t)__popcll(be);
+    uint32_t at = __builtin_amdgcn_readfirstlane((int)before), eq = __builtin_amdgcn_readfirstlane((int)eq_before);
+    at += min(eq, need);
+    // of 64 rows, `be` are equal to the cut and `eq` such rows lie before them: those that are still wanted, the lowest rows
+    auto wanted = [&](unsigned long long be) {
+        const uint32_t many = (uint32_t)__popcll(be);
+        for (uint32_t k = need - eq; k < many && be; ++k) be &= ~(1ull << (63 - __builtin_clzll(be)));
+        eq += many;
+        return be;
+    };
+    if constexpr (KEYS > 0) {
+        if (eq < need && equal > 0) {
+            if (eq + equal <= need) {
+                kept_rows |= equal_rows;
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < KEYS && eq < need; ++i) kept_rows |= (uint32_t)(wanted(__ballot((equal_rows >> i) & 1)) >> lane & 1) << i;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const bool mine = (kept_rows >> i) & 1;
+            const unsigned long long kept = __ballot(mine);
+            if (mine) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(kept >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)kept, 0u))] = s0 + i * 64 + lane;
+            at += (uint32_t)__popcll(kept);
+        }
+    } else {
+        each([&](int, int32_t j0, uint32_t key) {
+            unsigned long long kept = __ballot(key > prefix);
+            if (eq < need) kept |= wanted(__ballot(key == prefix && j0 + lane < s1));
+            if ((kept >> lane) & 1) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(kept >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)kept, 0u))] = j0 + lane;
+            at += (uint32_t)__popcll(kept);
+        });
     }
 }
 
 // ------------------------------------------------------------------------------------------------
-// Compaction: row j of a head becomes row keep_idx[j].  Bound by HBM: the kept rows in and out.  One block takes all rows of a (layer, sequence, head, K or V) in
-// ascending order, 128 at a time, reading a group before it writes it: a group's rows lie at or behind the place they go to, and those of later groups
-// behind everything written, so the same buffers may be input and output.  A block's new scale is the largest of the scales its rows come with; a code of
-// a smaller one is rounded again (exactly, but for what leaves the normal range).
+// Compaction: row j of a head becomes row keep_idx[j].  Bound by HBM: the kept rows in and out.  A block's new scale is the largest of the scales its rows come
+// with; a code of a smaller one is rounded again (exactly, but for what leaves the normal range).
+// A launch block takes `span` rows of one (layer, sequence, head, K or V) in ascending order, 128 at a time, eight lanes a row.  Where the outputs are the inputs `span` is all
+// of them: a group's rows lie at or behind the place they go to, those of later groups behind everything written, and every group is read before it is
+// written, so nothing is lost.  The rows of the next group and the list of the one behind are on their way while a group is written: a chain of three loads would
+// otherwise be waited for every 16 KB.
 // ------------------------------------------------------------------------------------------------
 constexpr int kCompactRows = 128;
 
@@ -686,13 +988,12 @@ struct CompactArgs {
     uint8_t *K_out, *V_out;
     float *ks_out, *vs_out, *acc_out;
     const int32_t *cu_tok, *keep_idx, *n_keep;
-    int32_t B, n_kv, T_total, n_scales, shift, keep;
+    int32_t B, n_kv, T_total, n_scales, shift, keep, span;
 };
 
 __global__ __launch_bounds__(kBlockThreads) void cache_compact_kernel(CompactArgs a) {
-    __shared__ int32_t s_src[kCompactRows];
-    __shared__ float s_scale[kCompactRows];
-    const int tid = threadIdx.x, r = tid >> 3, part = (tid & 7) * 16;
+    __shared__ __align__(16) float s_top[2][kBlockWaves];     // largest scale of a wave's 8 rows
+    const int tid = threadIdx.x, w = tid >> 6, r = tid >> 3, part = (tid & 7) * 16;
     const int64_t row = blockIdx.x;
     const int h = (int)(row % a.n_kv), b = (int)(row / a.n_kv % a.B);
     const int64_t head = row / a.n_kv / a.B * a.n_kv + h;
@@ -700,6 +1001,8 @@ __global__ __launch_bounds__(kBlockThreads) void cache_compact_kernel(CompactArg
     int32_t first, rows;
     region(a.cu_tok, b, a.T_total, &first, &rows);
     const int32_t m = min(min(max(a.n_keep[row], 0), a.keep), rows);
+    const int32_t begin = (int32_t)min((int64_t)blockIdx.z * a.span, (int64_t)m), end = a.span < m - begin ? begin + a.span : m;
+    if (begin >= end) return;
     const int32_t* idx = a.keep_idx + row * a.keep;
     const int64_t pool = head * a.T_total + first, slot0 = head * a.n_scales + (first >> a.shift) + b;
     const uint8_t* src = (is_v ? a.V : a.K) + pool * kHeadDim + part;
@@ -707,72 +1010,101 @@ __global__ __launch_bounds__(kBlockThreads) void cache_compact_kernel(CompactArg
     const float* sc = (is_v ? a.vs : a.ks) + slot0;
     float* sc_out = (is_v ? a.vs_out : a.ks_out) + slot0;
     const float least = __uint_as_float(27u << 23);
-    const int block = 1 << a.shift;
-    for (int32_t j0 = 0; j0 < m; j0 += kCompactRows) {
-        const int32_t j = j0 + r;
-        float w = 0.0f;
-        if (tid < kCompactRows) {
-            int32_t s = j0 + tid < m ? idx[j0 + tid] : -1;
-            if (s < 0 || s >= rows) s = -1;
-            s_src[tid] = s;
-            s_scale[tid] = s >= 0 ? sc[s >> a.shift] : least;
-            if (!is_v && a.acc && s >= 0) w = a.acc[pool + s];
+    const int waves = (1 << a.shift) / 8, w0 = w & ~(waves - 1);      // waves of a scale block, the first of this one's
+    const bool weigh = !is_v && a.acc && (tid & 7) == 0;
+
+    // entry j of the list, -1 behind its end or where it is none of the rows; loads are unconditional (one under a condition waits for those before it)
+    auto entry = [&](int32_t j) {
+        const int32_t s = idx[min(j, end - 1)];
+        return j < end && s >= 0 && s < rows ? s : -1;
+    };
+    struct Group { int32_t from; uint4 v; float scale, weight; };
+    auto load = [&](Group& g, int32_t from) {
+        const int32_t s = max(from, 0);
+        g.from = from;
+        g.v = ld_stream(src + (int64_t)s * kHeadDim);
+        g.scale = sc[s >> a.shift];
+        g.weight = weigh ? a.acc[pool + s] : 0.0f;
+    };
+    Group now, next;
+    load(now, entry(begin + r));
+    int32_t from = entry(begin + kCompactRows + r);
+    int buf = 0;
+    for (int32_t j0 = begin; j0 < end; j0 += kCompactRows, buf ^= 1) {
+        const bool more = j0 + kCompactRows < end;
+        if (more) {
+            load(next, from);
+            from = entry(j0 + 2 * kCompactRows + r);
         }
+        const float mine = now.from >= 0 ? now.scale : least;
+        float top = mine;
+        top = fmaxf(top, __shfl_xor(top, 8));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if ((tid & 63) == 0) s_top[buf][w] = top;
+        uint4 v = now.from >= 0 ? now.v : make_uint4(0, 0, 0, 0);
+        float weight = now.from >= 0 ? now.weight : 0.0f;
+        asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w), "+v"(weight));       // this group's loads have arrived before any of it is written
         __syncthreads();
-        const int32_t from = s_src[r];
-        uint4 v = from >= 0 ? *reinterpret_cast<const uint4*>(src + (int64_t)from * kHeadDim) : make_uint4(0, 0, 0, 0);
-        float top = least;
-        const int q0 = r & ~(block - 1);
-        for (int i = 0; i < block; ++i) top = fmaxf(top, s_scale[q0 + i]);
-        const float mine = s_scale[r];
+        for (int i = 0; i < waves; ++i) top = fmaxf(top, s_top[buf][w0 + i]);
         if (mine != top) {
             const float f = mine / top;
             v = make_uint4(rescale(v.x, f), rescale(v.y, f), rescale(v.z, f), rescale(v.w, f));
         }
-        block_sync_after_stores();                            // the loads have arrived before any row is written
-        if (j < m) {
-            *reinterpret_cast<uint4*>(dst + (int64_t)j * kHeadDim) = v;
-            if ((tid & 7) == 0 && r == q0) sc_out[j >> a.shift] = top;
+        const int32_t j = j0 + r;
+        if (j < end) {
+            st_stream(dst + (int64_t)j * kHeadDim, v);
+            if (weigh) a.acc_out[pool + j] = weight;
+            if ((tid & 7) == 0 && (j & ((1 << a.shift) - 1)) == 0) sc_out[j >> a.shift] = top;
         }
-        if (!is_v && a.acc_out && tid < kCompactRows && j0 + tid < m) a.acc_out[pool + j0 + tid] = w;
+        now = next;
     }
 }
 
 inline int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 inline int log2_of(int32_t n) { return 31 - __builtin_clz((unsigned)n); }
 
-// How skv_cache_attend cuts its work: blocks of `chunk` rows per (sequence, head) pair, and where the parts of the workspace begin.
-constexpr int kCacheWaves = 4;
+// How skv_cache_attend deals its work, and where the parts of the workspace begin.
+constexpr int kCacheRagged = 512;
 struct AttendPlan {
-    int32_t chunk, splits;
-    int64_t logit_stride, ml, lse2, logits, bytes;
+    int deal;
+    int32_t chunk, splits, blocks;         // kShare: blocks of the launch
+    int64_t logit_rows, ml, lse2, units, logits, bytes;
 };
 AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool weights) {
     AttendPlan p;
-    const int64_t pairs = (int64_t)B * c->d.n_kv_heads, heads = pairs * c->G;
-    const int32_t step = kCacheWaves * kCacheTile;
-    int64_t splits = (4 * (int64_t)c->n_cu + pairs - 1) / pairs, most = (max_n + step - 1) / step;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    int64_t chunk = round_up((max_n + splits - 1) / splits, step);
-    if (chunk < step) chunk = step;
-    if (listed && chunk > 1024) chunk = 1024;
+    const int64_t pairs = (int64_t)B * c->d.n_kv_heads, heads = pairs * c->G, rows = pairs * max_n;
+    const int64_t most = (int64_t)c->n_cu * (c->d.kv_dtype == SKV_BF16 && !weights ? 4 : 3);        // blocks that the chip holds at once
+    int64_t chunk = round_up((rows + most - 1) / most, kCacheStep);
+    if (chunk < kCacheStep) chunk = kCacheStep;
+    p.deal = listed ? kList : B > 1 && pairs <= kSharePairs && chunk > kCacheRagged / 2 ? kShare : kGrid;
+    if (p.deal == kGrid && B > 1 && chunk > kCacheRagged) {               // sequences of unlike lengths: several rounds of shorter blocks
+        chunk = round_up((rows + 4 * most - 1) / (4 * most), kCacheStep);
+        if (chunk < kCacheRagged) chunk = kCacheRagged;
+    }
+    if (listed && chunk > kListedChunk) chunk = kListedChunk;
     p.chunk = (int32_t)chunk;
     p.splits = (int32_t)((max_n + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
-    p.logit_stride = round_up(max_n, kCacheTile);
-    p.ml = round_up(p.splits > 1 ? heads * p.splits * kHeadDim * 4 : 0, 256);
-    p.lse2 = p.ml + round_up(p.splits > 1 ? heads * p.splits * 8 : 0, 256);
-    p.logits = p.lse2 + round_up(heads * 4, 256);
-    p.bytes = p.logits + (weights ? round_up(heads * p.logit_stride * 4, 256) : 0);
+    p.blocks = 3 * c->n_cu;
+    const int64_t slots = p.deal == kShare ? p.blocks + pairs : p.splits > 1 ? pairs * p.splits : 0;
+    p.logit_rows = round_up(max_n, kCacheTile);
+    p.ml = round_up(slots * c->G * kHeadDim * 4, 256);
+    p.lse2 = p.ml + round_up(slots * c->G * 8, 256);
+    p.units = p.lse2 + round_up(heads * 4, 256);
+    p.logits = p.units + round_up((pairs + 1) * 4, 256);
+    p.bytes = p.logits + (weights ? round_up(heads * p.logit_rows * 4, 256) : 0);
     return p;
 }
 
-template <int PIECES, bool LISTED, bool WEIGHTS>
-hipError_t attend_launch(Ctx* c, const CacheAttendArgs& a, int32_t pairs) {
-    size_t lds = (size_t)kCacheWaves * 8 * (2 + kHeadDim) * 4;
-    if (LISTED && (size_t)a.chunk * 12 > lds) lds = (size_t)a.chunk * 12;
-    hipLaunchKernelGGL((cache_attend_kernel<PIECES, LISTED, WEIGHTS, kCacheWaves>), dim3(a.splits, pairs), dim3(kCacheWaves * kWave), lds, c->stream, a);
+template <int PIECES, int DEAL, bool WEIGHTS>
+hipError_t attend_launch(Ctx* c, const CacheAttendArgs& a, int32_t blocks) {
+    size_t lds = (size_t)kCacheWaves * 8 * (2 + kHeadDim) * 4;                             // joining the waves
+    if (DEAL == kList && (size_t)a.chunk * 12 > lds) lds = (size_t)a.chunk * 12;
+    if (WEIGHTS && (size_t)kCacheWaves * a.G * kStageTiles * kCacheTile * 4 > lds) lds = (size_t)kCacheWaves * a.G * kStageTiles * kCacheTile * 4;
+    if (DEAL == kShare) lds += (size_t)(a.pairs + 4) / 4 * 16;
+    const dim3 grid = DEAL == kShare ? dim3(blocks) : dim3(a.splits, a.pairs);
+    hipLaunchKernelGGL((cache_attend_kernel<PIECES, DEAL, WEIGHTS>), grid, dim3(kCacheWaves * kWave), lds, c->stream, a);
     return hipGetLastError();
 }
 
@@ -785,10 +1117,16 @@ hipError_t launch_rotary(Ctx* c, int32_t n, const void* q, const void* k, const 
     const bool vec = rot % 16 == 0;
     RotArgs a{(const char*)q, (const char*)k, (char*)q_out, (char*)k_out, pos, inv_freq, n, q ? c->d.n_q_heads : 0, k ? c->d.n_kv_heads : 0, rot / 2, 0, mscale};
     const int heads = a.n_q + a.n_k, rows = vec ? (EB == 2 ? 8 : 4) : 1;
+    // Few tokens: as few heads a wave as one load takes, for a short chain.  Many: all heads of a token, so that its angles are formed once (32768 tokens of 40 bf16 heads: 110 us with
+    // one wave a token, 115 with two, 136 with five).  Between: as many waves as the chip has places for, 32 a compute unit.
     int groups = (heads + rows - 1) / rows;
+    const int64_t most = (32 * (int64_t)c->n_cu + n - 1) / n;
+    if (groups > most) groups = (int)most;
     if (groups > 65535) groups = 65535;
-    a.heads_per_wave = (heads + groups - 1) / groups;
-    const dim3 grid((n + kRotWaves - 1) / kRotWaves, groups), block(kRotWaves * kWave);
+    a.heads_per_wave = (int)round_up((heads + groups - 1) / groups, rows);
+    groups = (heads + a.heads_per_wave - 1) / a.heads_per_wave;
+    const int64_t blocks = ((int64_t)n + kRotWaves - 1) / kRotWaves;
+    const dim3 grid((unsigned)(blocks < 1 << 22 ? blocks : 1 << 22), groups), block(kRotWaves * kWave);
     auto go = [&](auto eb, auto il) {
         constexpr int E = decltype(eb)::value;
         constexpr bool I = decltype(il)::value;
@@ -807,8 +1145,10 @@ hipError_t launch_cache_append(Ctx* c, int32_t layer, int32_t B, const void* k, 
     const int H = c->d.n_kv_heads, n_scales = T_total / block + B;
     const int64_t pool = (int64_t)layer * H * T_total, sc = (int64_t)layer * H * n_scales;
     const AppendArgs a{(const char*)k, (const char*)v, (uint8_t*)K + pool * kHeadDim, (uint8_t*)V + pool * kHeadDim, ks + sc, vs + sc, acc ? acc + pool : nullptr,
-                       cu_new, cu_tok, n_tok, n_new, max_new, T_total, n_scales, log2_of(block), H};
-    const dim3 grid((unsigned)(((int64_t)max_new + block - 2) / block + 1), B * H, 2);
+                       cu_new, cu_tok, n_tok, n_new, max_new, T_total, n_scales, H};
+    // pairs fastest: a token's heads lie side by side in the input, and the blocks that read them run at the same time
+    const int64_t blocks = ((int64_t)max_new + block - 2) / block + 1;
+    const dim3 grid(B * H, (unsigned)(blocks < 65535 ? blocks : 65535), 2);
     auto go = [&](auto eb) {
         constexpr int E = decltype(eb)::value;
         switch (block) {
@@ -835,23 +1175,35 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
     const AttendPlan p = attend_plan(c, B, max_n, listed, weights);
     const int H = c->d.n_kv_heads, n_scales = T_total / block + B, pairs = B * H;
     const int64_t pool = (int64_t)layer * H * T_total, sc = (int64_t)layer * H * n_scales;
+    const bool share = p.deal == kShare, joined = share || p.splits > kJoinInside;
     char* ws = static_cast<char*>(work);
     const CacheAttendArgs a{(const char*)q, (const uint8_t*)K + pool * kHeadDim, (const uint8_t*)V + pool * kHeadDim, ks + sc, vs + sc, cu_tok, n_tok, tok_idx,
-                            max_n, T_total, n_scales, log2_of(block), H, c->G, p.chunk, p.splits, p.logit_stride, out, lse, (float*)ws, (float*)(ws + p.ml),
-                            weights ? (float*)(ws + p.lse2) : nullptr, (float*)(ws + p.logits)};
+                            max_n, T_total, n_scales, log2_of(block), H, c->G, pairs, p.chunk, p.splits, p.logit_rows, out, lse, (float*)ws, (float*)(ws + p.ml),
+                            weights ? (float*)(ws + p.lse2) : nullptr, (float*)(ws + p.logits), (int32_t*)(ws + p.units),
+                            !joined && p.splits > 1 ? c->att_counter : nullptr};
     hipError_t e;
-    if (listed) e = wide ? attend_launch<3, true, false>(c, a, pairs) : attend_launch<1, true, false>(c, a, pairs);
-    else if (weights) e = wide ? attend_launch<3, false, true>(c, a, pairs) : attend_launch<1, false, true>(c, a, pairs);
-    else e = wide ? attend_launch<3, false, false>(c, a, pairs) : attend_launch<1, false, false>(c, a, pairs);
+    if (listed) e = wide ? attend_launch<3, kList, false>(c, a, 0) : attend_launch<1, kList, false>(c, a, 0);
+    else if (share && weights) e = wide ? attend_launch<3, kShare, true>(c, a, p.blocks) : attend_launch<1, kShare, true>(c, a, p.blocks);
+    else if (share) e = wide ? attend_launch<3, kShare, false>(c, a, p.blocks) : attend_launch<1, kShare, false>(c, a, p.blocks);
+    else if (weights) e = wide ? attend_launch<3, kGrid, true>(c, a, 0) : attend_launch<1, kGrid, true>(c, a, 0);
+    else e = wide ? attend_launch<3, kGrid, false>(c, a, 0) : attend_launch<1, kGrid, false>(c, a, 0);
     if (e != hipSuccess) return e;
-    if (p.splits > 1) {
-        hipLaunchKernelGGL(cache_join_kernel, dim3(pairs * c->G), dim3(kHeadDim), 0, c->stream, a, listed ? 1 : 0);
+    if (joined) {
+        hipLaunchKernelGGL(cache_join_kernel, dim3(pairs * c->G, kHeadDim / kJoinDims), dim3(kJoinThreads), 0, c->stream, a, listed ? 1 : 0,
+                           share ? p.blocks : 0);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (weights && max_n > 0) {
-        hipLaunchKernelGGL(cache_weights_kernel, dim3((max_n + kWeightThreads - 1) / kWeightThreads, pairs), dim3(kWeightThreads), 0, c->stream, a,
-                           acc ? acc + pool : nullptr, acc_out + pool, decay);
+        const int per = kWeightThreads * kWeightRows;
+        const dim3 grid((max_n + per - 1) / per, pairs), block(kWeightThreads);
+        const float* from = acc ? acc + pool : nullptr;
+        switch (c->G) {
+            case 1: hipLaunchKernelGGL(cache_weights_kernel<1>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
+            case 2: hipLaunchKernelGGL(cache_weights_kernel<2>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
+            case 4: hipLaunchKernelGGL(cache_weights_kernel<4>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
+            default: hipLaunchKernelGGL(cache_weights_kernel<8>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
+        }
         e = hipGetLastError();
     }
     return e;
@@ -860,7 +1212,10 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
 hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_total, const int32_t* cu_tok, const int32_t* n_tok, int32_t max_n, int32_t keep,
                               int32_t sink, int32_t recent, int32_t* keep_idx, int32_t* n_keep) {
     const EvictArgs a{acc, cu_tok, n_tok, B, c->d.n_kv_heads, T_total, max_n, keep, sink, recent, keep_idx, n_keep};
-    hipLaunchKernelGGL(cache_evict_kernel, dim3(c->d.n_layers * B * c->d.n_kv_heads), dim3(kBlockThreads), 0, c->stream, a);
+    const dim3 grid(c->d.n_layers * B * c->d.n_kv_heads), threads(kBlockThreads);
+    if (max_n <= 8 * kBlockThreads) hipLaunchKernelGGL(cache_evict_kernel<8>, grid, threads, 0, c->stream, a);
+    else if (max_n <= 32 * kBlockThreads) hipLaunchKernelGGL(cache_evict_kernel<32>, grid, threads, 0, c->stream, a);
+    else hipLaunchKernelGGL(cache_evict_kernel<0>, grid, threads, 0, c->stream, a);
     return hipGetLastError();
 }
 
@@ -868,9 +1223,17 @@ hipError_t launch_cache_compact(Ctx* c, int32_t B, const void* K, const void* V,
                                 const int32_t* cu_tok, const int32_t* keep_idx, int32_t keep, const int32_t* n_keep, void* K_out, void* V_out, float* ks_out,
                                 float* vs_out, float* acc_out) {
     if (keep == 0) return hipSuccess;
+    const int64_t heads = (int64_t)c->d.n_layers * B * c->d.n_kv_heads;
+    // other outputs: rows cut over blocks until there are four for every place on the chip (two blocks a compute unit), in groups of 128
+    int32_t span = keep;
+    if (K != K_out) {
+        const int64_t cuts = (8 * (int64_t)c->n_cu + 2 * heads - 1) / (2 * heads);
+        span = (int32_t)round_up((keep + cuts - 1) / cuts, kCompactRows);
+        if ((keep + span - 1) / span > 65535) span = (int32_t)round_up((keep + 65534) / 65535, kCompactRows);
+    }
     const CompactArgs a{(const uint8_t*)K, (const uint8_t*)V, ks, vs, acc, (uint8_t*)K_out, (uint8_t*)V_out, ks_out, vs_out, acc_out, cu_tok, keep_idx, n_keep,
-                        B, c->d.n_kv_heads, T_total, T_total / block + B, log2_of(block), keep};
-    hipLaunchKernelGGL(cache_compact_kernel, dim3(c->d.n_layers * B * c->d.n_kv_heads, 2), dim3(kBlockThreads), 0, c->stream, a);
+                        B, c->d.n_kv_heads, T_total, T_total / block + B, log2_of(block), keep, span};
+    hipLaunchKernelGGL(cache_compact_kernel, dim3((unsigned)heads, 2, (unsigned)((keep + span - 1) / span)), dim3(kBlockThreads), 0, c->stream, a);
     return hipGetLastError();
 }
 

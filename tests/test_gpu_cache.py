@@ -238,12 +238,12 @@ def check_attend(ref, layer, q, n, out, lse, idx=None, acc=None, decay=1.0, acc_
             K, V = (ref.rows(kv, layer, h, b, rows) for kv in range(2))
             want, wl, p, l1 = R.attend(q[b, h * G:(h + 1) * G], K, V)
             # A logit: 128 products and their fp32 sum (fp32 queries: three pieces, 384), scale and 1 / sqrt(D): (384 + 4) half steps of the sum of |products|.  A weight:
-            # twice that (numerator and normaliser), the exponent's own rounding and exp2, 2^-18 for its 16 bits; sums over the rows of a wave and over waves and blocks.
+            # twice that (numerator and normaliser), the exponent's own rounding and exp2; sums over the rows of a wave and over waves and blocks.
             logit = 388 * EPS * l1
             weight = 2 * logit + 2 * (abs(wl).max() if len(rows) else 0.0) * 4 * EPS + 8 * EPS + (len(rows) / 32 + 300) * EPS
             size = np.stack([(p[g][:, None] * np.abs(V)).sum(0) for g in range(G)]) if len(rows) else 0.0
             got, gl = out[b, h * G:(h + 1) * G], lse[b, h * G:(h + 1) * G]
-            assert np.all(np.abs(got - want) <= 2 * (weight + 2.0 ** -18) * size + 1e-30), (b, h, np.abs(got - want).max())
+            assert np.all(np.abs(got - want) <= 2 * weight * size + 1e-30), (b, h, np.abs(got - want).max())
             if len(rows):
                 assert np.all(np.abs(gl - wl) <= logit + weight + 4 * EPS * np.abs(wl)), (b, h)
             else:
@@ -302,6 +302,46 @@ def test_attend_gathers_the_weights(lengths, H, G, dtype, block):
         for h in range(H):
             used[1, h, ref.cu[b]: ref.cu[b] + int(n[b][h])] = True
     assert torch.equal(inplace[used], acc_out[used]) and torch.equal(inplace[~used], dev["acc"][~used])
+
+
+@pytest.mark.parametrize("lengths", [(1, 0, 700, 33), (0, 0, 0), (0, 5000, 1, 0, 129), (128, 128, 128), (4097, 300)])
+@pytest.mark.parametrize("H,G,dtype,block", [(1, 1, "bf16", 16), (2, 8, "bf16", 32), (3, 4, "f32", 64)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attend_deals_long_batches_in_equal_shares(lengths, H, G, dtype, block, weights):
+    """The bound on the lengths says that a batch is long: blocks then take equal shares of all rows, whatever the lengths are (some more blocks than rows)."""
+    rng, ref, dev, ctx, q = attend_case(sum(lengths) + 7 * G, lengths, H, G, dtype, block)
+    n = np.array([[x, max(0, x - 1), max(0, x - 9)][:H] for x in lengths])
+    acc_out = torch.rand(ref.acc.shape, device=DEV) if weights else None
+    before = f64(acc_out) if weights else None
+    out, lse = run_attend(ref, dev, ctx, 1, q, i32(n), 400000, acc=dev["acc"] if weights else None, acc_out=acc_out, decay=0.5)
+    check_attend(ref, 1, q, n, out, lse, acc=ref.acc, decay=0.5, acc_out=(before, f64(acc_out)) if weights else None)
+    again = run_attend(ref, dev, ctx, 1, q, i32(n), 400000)
+    if not weights:
+        assert np.array_equal(out, again[0]) and np.array_equal(lse, again[1])
+
+
+def test_attend_more_pairs_than_equal_shares_are_dealt_for():
+    lengths = tuple(int(x) for x in np.random.RandomState(0).randint(0, 200, 600))
+    rng, ref, dev, _, q = attend_case(1, lengths, 2, 1, "bf16", 32, L=1)
+    ctx = context(H=2, G=1, batch=600)
+    n = np.array([[x, x // 2] for x in lengths])
+    for max_n in (200, 3000):
+        acc_out = torch.rand(ref.acc.shape, device=DEV)
+        before = f64(acc_out)
+        out, lse = run_attend(ref, dev, ctx, 0, q, i32(n), max_n, acc=dev["acc"], acc_out=acc_out)
+        check_attend(ref, 0, q, n, out, lse, acc=ref.acc, acc_out=(before, f64(acc_out)))
+
+
+def test_attend_of_many_rows_of_one_sequence():
+    """More parts than the attention launch joins itself, and scores of more tiles than a wave keeps."""
+    rng, ref, dev, ctx, q = attend_case(3, (70001,), 1, 2, "bf16", 128, L=1)
+    acc_out = torch.rand(ref.acc.shape, device=DEV)
+    before = f64(acc_out)
+    n = np.array([[70001]])
+    out, lse = run_attend(ref, dev, ctx, 0, q, i32(n), 70001, acc=dev["acc"], acc_out=acc_out, decay=0.25)
+    check_attend(ref, 0, q, n, out, lse, acc=ref.acc, decay=0.25, acc_out=(before, f64(acc_out)))
+    two, _ = run_attend(ref, dev, ctx, 0, q, i32(n), 70001)
+    check_attend(ref, 0, q, n, two, lse)
 
 
 @pytest.mark.parametrize("length,listed", [(40, 1), (40, 40), (900, 129), (5000, 2048), (5000, 1027)])
@@ -399,7 +439,7 @@ def test_attend_large_and_small_magnitudes(shift):
         for h in range(2):
             K, V = (ref.rows(kv, 1, h, b, np.arange(n[b, h])) for kv in range(2))
             want, wl, p, l1 = R.attend(f64(q)[b, h * 4:(h + 1) * 4], K, V)
-            d = math.expm1(2 * 388 * EPS * l1 + 8 * EPS * l1) + 2.0 ** -17 + 400 * EPS
+            d = math.expm1(2 * 388 * EPS * l1 + 8 * EPS * l1) + 400 * EPS
             size = np.stack([(p[g][:, None] * np.abs(V)).sum(0) for g in range(4)])
             # and numbers below 2^-126, the smallest normal one, may count as zero: a weight times its scale, which meets codes of up to 448, in every row
             gone = 448 * 2.0 ** -126 * n[b, h]
