@@ -347,8 +347,11 @@ __device__ __forceinline__ void store_out(const CacheAttendArgs& a, int64_t qi, 
 }
 
 // PIECES: bf16 pieces of a query (1: bf16 queries, 3: fp32).  kList: the chunk's rows and their scales lie in LDS.  WEIGHTS: the scores are kept for the last launch.
+// Blocks of four waves that a compute unit holds, by the registers of each form.
+constexpr int cache_places(int pieces, int deal, bool weights) { return pieces == 1 ? (deal == kShare || weights ? 3 : 4) : deal == kShare ? 2 : 3; }
+
 template <int PIECES, int DEAL, bool WEIGHTS>
-__global__ __launch_bounds__(kCacheWaves * kWave, PIECES == 1 && DEAL != kShare && !WEIGHTS ? 4 : 3) void cache_attend_kernel(CacheAttendArgs a) {
+__global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEIGHTS)) void cache_attend_kernel(CacheAttendArgs a) {
     extern __shared__ __align__(16) char smem_all[];
     constexpr bool LISTED = DEAL == kList;
     constexpr int kThreads = kCacheWaves * kWave;
@@ -475,13 +478,15 @@ __global__ __launch_bounds__(kCacheWaves * kWave, PIECES == 1 && DEAL != kShare 
     float sk[2], sv2[2];                                      // rows: the scales of the tile's two groups of 16 (blocks are multiples of 16)
 
     // A tile's scales are asked for with its keys: loads return in order, so that scales asked for later would be waited for with everything before them.
+    // Values come by non-temporal loads (2.4 M rows in plain ones 130 us, in these 124), keys by plain ones: a load takes half of a line, and the other one may be lost between
+    // non-temporal ones (32 lists of 2048 rows 33 us, with plain ones 28).
     auto load_k = [&](int32_t j /* first entry of the tile, in the piece */) {
         if (LISTED) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint8_t* p = Kh + (int64_t)max(l_idx[min(j + 16 * i + c, a.chunk - 1)], 0) * kHeadDim + 16 * g;
-                kt[2 * i] = ld_stream(p);
-                kt[2 * i + 1] = ld_stream(p + 64);
+                kt[2 * i] = *reinterpret_cast<const uint4*>(p);
+                kt[2 * i + 1] = *reinterpret_cast<const uint4*>(p + 64);
             }
             return;
         }
@@ -495,7 +500,7 @@ __global__ __launch_bounds__(kCacheWaves * kWave, PIECES == 1 && DEAL != kShare 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t off = (uint32_t)min(16 * i + c, count - 1 - j) * kHeadDim + 16 * g;
-            kt[2 * i] = *reinterpret_cast<const uint4*>(base + off);          // halves of a line: a non-temporal load of one may lose the other
+            kt[2 * i] = *reinterpret_cast<const uint4*>(base + off);
             kt[2 * i + 1] = *reinterpret_cast<const uint4*>(base + off + 64);
         }
     };
@@ -708,27 +713,42 @@ __global__ __launch_bounds__(kCacheWaves * kWave, PIECES == 1 && DEAL != kShare 
     }
     __syncthreads();
     if (!s_last) return;
-    float2* s_ml = reinterpret_cast<float2*>(smem);           // [parts][G], at most 8 * kJoinInside
+    // Everything is asked for at once: the references (through LDS, for all) and the first kJoinFirst sums of the two dims of up to two heads that a thread adds up.
+    float2* s_ml = reinterpret_cast<float2*>(smem);           // [parts][G], at most 8 * kJoinInside = the threads
+    constexpr int kJoinFirst = 16, kItems = 8 * (kHeadDim / 2) / kThreads;
     const int64_t pi0 = (int64_t)pair * a.splits * G;
-    for (int e = tid; e < G * parts; e += kThreads) {
-        const unsigned long long v = ld_agent64(a.ml + 2 * (pi0 + e));
-        s_ml[e] = make_float2(lo_f(v), hi_f(v));
-    }
+    const unsigned long long m_own = ld_agent64(a.ml + 2 * (pi0 + min(tid, G * parts - 1)));
+    unsigned long long v[kItems][kJoinFirst];
+    auto sums = [&](int k) {                                  // of the thread's item k
+        const int e = min(tid + k * kThreads, G * (kHeadDim / 2) - 1);
+        return a.part + (pi0 + e / (kHeadDim / 2)) * kHeadDim + e % (kHeadDim / 2) * 2;
+    };
+#pragma unroll
+    for (int k = 0; k < kItems; ++k)
+        if (k * kThreads < G * (kHeadDim / 2)) {
+#pragma unroll
+            for (int i = 0; i < kJoinFirst; ++i) v[k][i] = ld_agent64(sums(k) + (int64_t)min(i, parts - 1) * G * kHeadDim);
+        }
+    if (tid < G * parts) s_ml[tid] = make_float2(lo_f(m_own), hi_f(m_own));
     __syncthreads();
-    for (int e = tid; e < G * (kHeadDim / 2); e += kThreads) {
-        const int qg = e / (kHeadDim / 2), d = e % (kHeadDim / 2) * 2;
-        const float* part = a.part + (pi0 + qg) * kHeadDim + d;
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+        const int e = tid + k * kThreads, qg = e / (kHeadDim / 2), d = e % (kHeadDim / 2) * 2;
+        if (e >= G * (kHeadDim / 2)) break;
         float top = neg_inf, z = 0.0f, s0 = 0.0f, s1 = 0.0f;
         for (int i = 0; i < parts; ++i) top = fmaxf(top, s_ml[i * G + qg].x);
         const float top0 = top == neg_inf ? 0.0f : top;
-#pragma unroll 8
-        for (int i = 0; i < parts; ++i) {
-            const unsigned long long v = ld_agent64(part + (int64_t)i * G * kHeadDim);
-            const float f = __builtin_amdgcn_exp2f(s_ml[i * G + qg].x - top0);
-            z += f * s_ml[i * G + qg].y;
-            s0 += f * lo_f(v);
-            s1 += f * hi_f(v);
-        }
+        auto add = [&](int i, unsigned long long p) {
+            const float2 m = s_ml[i * G + qg];
+            const float f = __builtin_amdgcn_exp2f(m.x - top0);
+            z += f * m.y;
+            s0 += f * lo_f(p);
+            s1 += f * hi_f(p);
+        };
+#pragma unroll
+        for (int i = 0; i < kJoinFirst; ++i)
+            if (i < parts) add(i, v[k][i]);
+        for (int i = kJoinFirst; i < parts; ++i) add(i, ld_agent64(sums(k) + (int64_t)i * G * kHeadDim));
         const int64_t qi = (int64_t)pair * G + qg;
         store_out(a, qi, d, s0, z, top0);
         store_out(a, qi, d + 1, s1, z, top0);
@@ -1074,7 +1094,8 @@ struct AttendPlan {
 AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool weights) {
     AttendPlan p;
     const int64_t pairs = (int64_t)B * c->d.n_kv_heads, heads = pairs * c->G, rows = pairs * max_n;
-    const int64_t most = (int64_t)c->n_cu * (c->d.kv_dtype == SKV_BF16 && !weights ? 4 : 3);        // blocks that the chip holds at once
+    const int pieces = c->d.kv_dtype == SKV_BF16 ? 1 : 3;
+    const int64_t most = (int64_t)c->n_cu * cache_places(pieces, kGrid, weights);        // blocks that the chip holds at once
     int64_t chunk = round_up((rows + most - 1) / most, kCacheStep);
     if (chunk < kCacheStep) chunk = kCacheStep;
     p.deal = listed ? kList : B > 1 && pairs <= kSharePairs && chunk > kCacheRagged / 2 ? kShare : kGrid;
@@ -1086,7 +1107,7 @@ AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool
     p.chunk = (int32_t)chunk;
     p.splits = (int32_t)((max_n + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
-    p.blocks = 3 * c->n_cu;
+    p.blocks = cache_places(pieces, kShare, weights) * c->n_cu;
     const int64_t slots = p.deal == kShare ? p.blocks + pairs : p.splits > 1 ? pairs * p.splits : 0;
     p.logit_rows = round_up(max_n, kCacheTile);
     p.ml = round_up(slots * c->G * kHeadDim * 4, 256);
