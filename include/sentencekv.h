@@ -351,8 +351,9 @@ int skv_rotary(skv_ctx* ctx, int32_t n, const void* q, const void* k, const int3
  *     k_scale, v_scale  dev [L][Hkv][T_total / block + B] fp32 (integer division)
  *     cu_tok            dev [B + 1]: sequence b has the rows cu_tok[b] .. cu_tok[b + 1] - 1 to itself, used from the first on.  Its block t (rows t * block .. of the
  *                       sequence, so that no block has rows of two) has its scale at cu_tok[b] / block + b + t.
- *     n_tok             dev [B][Hkv], 4-byte aligned (a slice of an array of all layers will do): rows in use of each sequence and head
+ *     n_tok             dev [B][Hkv]: rows in use of each sequence and head
  *     acc               dev [L][Hkv][T_total] fp32: attention weight gathered by each row
+ * n_tok, scales and acc need be aligned to 4 bytes only (slices of larger arrays will do).
  * All calls on a cache pass the same B, T_total and block.  What cu_tok, n_tok, counts and lists say is cut to the rows that a sequence has, never followed out of
  * the pool; rows that no call names are left as they were.
  * Scales are powers of two: the smallest s >= 2^-100 with |x| <= 448 s for the finite x of a block (E4M3 is a floating format: a scale between two powers would gain

@@ -49,7 +49,9 @@ inline int sv_bytes(const Ctx& c) { return c.d.semvec_dtype == SKV_BF16 ? 2 : c.
 
 
 // ---- the 8-bit cache --------------------------------------------------------------------------------------------------
-inline bool aligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// counts, scales and gathered weights are read word by word: slices of larger arrays will do
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool bad_words(const void* p) { return p == nullptr || !aligned4(p); }
 inline bool cache_block(int32_t block) { return block == 16 || block == 32 || block == 64 || block == 128; }
 
 // ---- skv_segment's wait for the number of sentences ---------------------------------------------------------------------
@@ -667,7 +669,7 @@ int skv_cache_append(skv_ctx* ctx, int32_t layer, int32_t B, const void* k, cons
                      const int32_t* cu_tok, const int32_t* n_tok, void* K, void* V, float* k_scale, float* v_scale, int32_t T_total, int32_t block, float* acc) {
     if (!ctx) return SKV_EINVAL;
     if (layer < 0 || layer >= ctx->c.d.n_layers || B < 1 || T_total < 1 || n_new < 0 || max_new < 0 || !cache_block(block)) return SKV_EINVAL;
-    if (bad_ptr(cu_new) || bad_ptr(cu_tok) || !aligned4(n_tok) || bad_ptr(K) || bad_ptr(V) || bad_ptr(k_scale) || bad_ptr(v_scale) || !aligned16(acc)) return SKV_EINVAL;
+    if (bad_ptr(cu_new) || bad_ptr(cu_tok) || bad_words(n_tok) || bad_ptr(K) || bad_ptr(V) || bad_words(k_scale) || bad_words(v_scale) || !aligned4(acc)) return SKV_EINVAL;
     if (n_new > 0 && (bad_ptr(k) || bad_ptr(v))) return SKV_EINVAL;
     if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens || n_new > ctx->c.d.max_tokens) return SKV_ECAPACITY;
     const int rc = check_ctx(ctx);
@@ -686,9 +688,9 @@ int skv_cache_attend(skv_ctx* ctx, int32_t layer, int32_t B, const void* q, cons
                      float* acc_out, float decay, void* work, int64_t work_bytes) {
     if (!ctx) return SKV_EINVAL;
     if (layer < 0 || layer >= ctx->c.d.n_layers || B < 1 || T_total < 1 || max_n < 0 || !cache_block(block)) return SKV_EINVAL;
-    if (bad_ptr(q) || bad_ptr(K) || bad_ptr(V) || bad_ptr(k_scale) || bad_ptr(v_scale) || bad_ptr(cu_tok) || !aligned4(n_tok) || bad_ptr(out) || bad_ptr(work))
+    if (bad_ptr(q) || bad_ptr(K) || bad_ptr(V) || bad_words(k_scale) || bad_words(v_scale) || bad_ptr(cu_tok) || bad_words(n_tok) || bad_ptr(out) || bad_ptr(work))
         return SKV_EINVAL;
-    if (!aligned16(tok_idx) || !aligned16(lse) || !aligned16(acc) || !aligned16(acc_out)) return SKV_EINVAL;
+    if (!aligned16(tok_idx) || !aligned16(lse) || !aligned4(acc) || !aligned4(acc_out)) return SKV_EINVAL;
     if ((acc_out && tok_idx) || (acc && !acc_out) || !(decay >= 0.0f && decay <= 1.0f)) return SKV_EINVAL;
     if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens || max_n > ctx->c.d.max_tokens) return SKV_ECAPACITY;
     if (work_bytes < skv::cache_attend_work_bytes(&ctx->c, B, max_n, acc_out != nullptr)) return SKV_EINVAL;
@@ -702,7 +704,7 @@ int skv_cache_evict(skv_ctx* ctx, int32_t B, const float* acc, int32_t T_total, 
                     int32_t recent, int32_t* keep_idx, int32_t* n_keep) {
     if (!ctx) return SKV_EINVAL;
     if (B < 1 || T_total < 1 || max_n < 0 || keep < 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > keep) return SKV_EINVAL;
-    if (bad_ptr(acc) || bad_ptr(cu_tok) || bad_ptr(n_tok) || bad_ptr(keep_idx) || bad_ptr(n_keep)) return SKV_EINVAL;
+    if (bad_words(acc) || bad_ptr(cu_tok) || bad_words(n_tok) || bad_ptr(keep_idx) || bad_ptr(n_keep)) return SKV_EINVAL;
     if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens || max_n > ctx->c.d.max_tokens) return SKV_ECAPACITY;
     const int rc = check_ctx(ctx);
     if (rc != SKV_OK) return rc;
@@ -714,8 +716,8 @@ int skv_cache_compact(skv_ctx* ctx, int32_t B, const void* K, const void* V, con
                       float* acc_out) {
     if (!ctx) return SKV_EINVAL;
     if (B < 1 || T_total < 1 || keep < 0 || !cache_block(block)) return SKV_EINVAL;
-    if (bad_ptr(K) || bad_ptr(V) || bad_ptr(k_scale) || bad_ptr(v_scale) || bad_ptr(cu_tok) || bad_ptr(keep_idx) || bad_ptr(n_keep) || bad_ptr(K_out) || bad_ptr(V_out) ||
-        bad_ptr(k_scale_out) || bad_ptr(v_scale_out) || !aligned16(acc) || !aligned16(acc_out) || (acc != nullptr) != (acc_out != nullptr))
+    if (bad_ptr(K) || bad_ptr(V) || bad_words(k_scale) || bad_words(v_scale) || bad_ptr(cu_tok) || bad_ptr(keep_idx) || bad_ptr(n_keep) || bad_ptr(K_out) || bad_ptr(V_out) ||
+        bad_words(k_scale_out) || bad_words(v_scale_out) || !aligned4(acc) || !aligned4(acc_out) || (acc != nullptr) != (acc_out != nullptr))
         return SKV_EINVAL;
     const int same = (K == K_out) + (V == V_out) + (k_scale == k_scale_out) + (v_scale == v_scale_out);
     if ((same != 0 && same != 4) || (acc && (acc == acc_out) != (same == 4))) return SKV_EINVAL;

@@ -101,10 +101,11 @@ for _name, _good in GOOD.items():
         if _good[_arg] == P:
             optional = (_name, _arg) in (("skv_cache_append", "acc"), ("skv_cache_attend", "lse"), ("skv_cache_attend", "acc"))
             CASES.append((_name, {_arg: None}, PASSES if optional else INVALID))
-            if _arg != "n_tok" or _name == "skv_cache_evict":
+            if _arg not in ("n_tok", "k_scale", "v_scale", "acc", "k_scale_out", "v_scale_out", "acc_out"):
                 CASES.append((_name, {_arg: P + 8}, INVALID))
             else:
-                CASES += [(_name, {_arg: P + 4}, PASSES), (_name, {_arg: P + 2}, INVALID)]
+                together = {x: P + 4 for x in (_arg, _arg.removesuffix("_out"), _arg + "_out") if x in _good and _name == "skv_cache_compact"} or {_arg: P + 4}
+                CASES += [(_name, together, PASSES), (_name, {_arg: P + 2}, INVALID)]
 CASES += [("skv_rotary", kw, want) for kw, want in [
     (dict(n=-1), INVALID), (dict(n=1001), CAPACITY), (dict(rot=0), INVALID), (dict(rot=63), INVALID), (dict(rot=130), INVALID), (dict(interleaved=2), INVALID),
     (dict(mscale=NAN), INVALID), (dict(mscale=math.inf), INVALID), (dict(q=None, q_out=None), PASSES), (dict(k=None, k_out=None), PASSES),

@@ -407,6 +407,35 @@ def test_attend_counts_and_offsets_are_cut_to_the_pool():
     assert torch.equal(before, acc_out)
 
 
+def test_scales_weights_and_counts_may_begin_at_any_word():
+    rng, ref, dev, ctx, q = attend_case(21, (300, 77), 3, 2, "bf16", 32)
+    n = np.array([[300, 299, 3], [77, 0, 1]])
+
+    def moved(x):
+        y = torch.zeros(x.numel() + 5, dtype=x.dtype, device=DEV)
+        y[5:] = x.flatten()
+        return y[5:].view(x.shape)
+
+    want = run_attend(ref, dev, ctx, 1, q, i32(n), 300, acc=dev["acc"], acc_out=(a := torch.zeros_like(dev["acc"])))
+    m = dict(dev, ks=moved(dev["ks"]), vs=moved(dev["vs"]))
+    got = run_attend(ref, m, ctx, 1, q, moved(i32(n)), 300, acc=moved(dev["acc"]), acc_out=(b := moved(torch.zeros_like(a))))
+    assert np.array_equal(want[0], got[0]) and np.array_equal(want[1], got[1]) and torch.equal(a, b)
+    m["acc"] = moved(dev["acc"])
+    k = torch.randn(5, 3, D).bfloat16()
+    run_append(ref, m, ctx, 1, n, [3, 2], k, 4 * k, moved(i32(n)), ref.T)
+    check_cache(m, ref)
+    idx, n_keep = torch.zeros(2, 2, 3, 9, dtype=torch.int32, device=DEV), torch.zeros(2, 2, 3, dtype=torch.int32, device=DEV)
+    ctx.cache_evict(2, m["acc"], ref.T, m["cu"], moved(i32([n, n])), 300, 9, 2, 3, idx, n_keep)
+    for l in range(2):
+        for b in range(2):
+            for h in range(3):
+                at = R.evict(ref.acc[l, h, ref.cu[b]: ref.cu[b] + n[b, h]].astype(np.float32), 9, 2, 3)
+                assert np.array_equal(idx[l, b, h, : len(at)].cpu().numpy(), at)
+                ref.compact(l, b, h, at)
+    ctx.cache_compact(2, m["K"], m["V"], m["ks"], m["vs"], m["acc"], ref.T, 32, m["cu"], idx, 9, n_keep, m["K"], m["V"], m["ks"], m["vs"], m["acc"])
+    check_cache(m, ref)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_special_logits(dtype):
     rng, ref, dev, ctx, q = attend_case(9, (200,), 2, 2, dtype, 64)
