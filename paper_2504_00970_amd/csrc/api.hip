@@ -80,7 +80,7 @@ int32_t wait_for_count(Ctx& c) {
 
 // ---- workspace: one block of device memory, carved the same way whether skv_create allocated it or it is the static
 // scratch array of skv_decode_step_noalloc ---------------------------------------------------------------------------
-constexpr int kWsParts = 17;
+constexpr int kWsParts = 18;
 // Fixed sizes of the tagged area (epochs, tagged scores, tagged partials) in the static scratch of
 // skv_decode_step_noalloc: that area must hold tagged words only, whatever descriptor a call brings (a word of some
 // other array could look like a valid tag), so it has the same extent for every descriptor.
@@ -125,6 +125,7 @@ size_t workspace_layout(const skv_desc& d, int max_splits, int max_sel, bool fix
     sz[14] = sweeps ? (size_t)skv::kSweepMaxBlocks * skv::kSweepMaxRows * sizeof(unsigned long long) : 0;                  // imp_part
     sz[15] = sweeps ? stat_heads * skv::kSweepMaxRows * sizeof(unsigned long long) : 0;                                    // imp_stat
     sz[16] = fixed_tagged || d.n_layers > skv::kRetMaxLayers || d.max_tokens <= skv::kRetainLongTok ? 0 : round256((size_t)d.n_layers * kRetainLayerBytes);
+    sz[17] = fixed_tagged ? 0 : (size_t)skv::evict_slices(d) * skv::kEvictSliceWords * 4;
     size_t total = 0;
     for (int i = 0; i < kWsParts; ++i) total += sz[i];
     return total;
@@ -161,6 +162,7 @@ void carve_workspace(Ctx& c, char* base, const size_t sz[kWsParts], int32_t scor
         c.ret_count = reinterpret_cast<unsigned int*>(c.ret_cut + 4 * L);
     }
     p += sz[16];
+    c.evict_counts = sz[17] ? reinterpret_cast<unsigned int*>(p) : nullptr; p += sz[17];
     c.imp_part_words = (int64_t)(sz[14] / sizeof(unsigned long long));
     c.imp_stat_words = (int64_t)(sz[15] / sizeof(unsigned long long));
 }

@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 // a lane, once per wave.  A wave takes one token and some of its heads; a lane turns two 16-byte pieces of a row, whose partners lie in one
 // another (half layout) or in themselves (interleaved), so that a row may be turned where it lies.
 // ------------------------------------------------------------------------------------------------
-constexpr int kRotWaves = 4;
+constexpr int kRotWaves = 4, kRotRows = 4;
 
 struct RotArgs {
     const char *q, *k;
@@ -80,7 +80,7 @@ template <int EB> __device__ __forceinline__ uint4 pack16(const float* f) {
     else return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
 }
 
-// VEC: rot is a multiple of 16.  Otherwise a lane turns one pair, element by element.  A wave's table of cosines and sines is its own: no barrier.
+// VEC: rot is a multiple of 16.  Otherwise lanes hold neighbouring elements, whatever their partners are.  A wave's table of cosines and sines is its own: no barrier.
 template <int EB, bool INTERLEAVED, bool VEC>
 __global__ __launch_bounds__(kRotWaves * kWave) void rotary_kernel(RotArgs a) {
     __shared__ __align__(16) float2 table[kRotWaves][kHeadDim / 2];
@@ -144,31 +144,72 @@ __global__ __launch_bounds__(kRotWaves * kWave) void rotary_kernel(RotArgs a) {
                 if (hb + ROWS < h1) load(h + ROWS);
             }
         } else {
+            // a lane has the elements 2 lane and 2 lane + 1 of kRotRows rows; partners that lie in other lanes (half layout) are read from LDS
+            using Word = std::conditional_t<EB == 2, uint32_t, uint2>;
+            __shared__ __align__(16) float rows[INTERLEAVED ? 1 : kRotWaves][kRotRows][kHeadDim];
+            Word word[kRotRows];
+            auto load = [&](int h) {                          // past the last head: the last one again, which is not stored
+#pragma unroll
+                for (int r = 0; r < kRotRows; ++r) word[r] = *reinterpret_cast<const Word*>(row_in(min(h + r, heads - 1)) + 2 * EB * lane);
+            };
+            load(h0);
             angles();
-            const bool turn = lane < a.half;
-            const int ea = turn && !INTERLEAVED ? lane : 2 * lane, eb = turn && !INTERLEAVED ? lane + a.half : 2 * lane + 1;
-            const float2 t = turn ? table[w][lane] : make_float2(1.0f, 0.0f);
-            for (int h = h0; h < h1; ++h) {
-                const char* in = row_in(h);
-                char* out = row_out(h);
-                if constexpr (EB == 2) {
-                    const uint16_t* i16 = reinterpret_cast<const uint16_t*>(in);
-                    uint16_t* o16 = reinterpret_cast<uint16_t*>(out);
-                    uint32_t xa = i16[ea], xb = i16[eb];
-                    if (turn) {
-                        const float x = __uint_as_float(xa << 16), y = __uint_as_float(xb << 16);
-                        const uint32_t z = bf16_pair(x * t.x - y * t.y, y * t.x + x * t.y);
-                        xa = z & 0xffffu;
-                        xb = z >> 16;
+            // y = x * c + partner * s
+            float c[2], s[2];
+            int partner[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int e = 2 * lane + i;
+                const bool turn = e < 2 * a.half, upper = INTERLEAVED ? i == 1 : e >= a.half;
+                const float2 t = turn ? table[w][INTERLEAVED ? lane : upper ? e - a.half : e] : make_float2(1.0f, 0.0f);
+                c[i] = t.x;
+                s[i] = upper ? t.y : -t.y;
+                partner[i] = !turn ? e : upper ? e - a.half : e + a.half;
+            }
+            for (int h = h0; h < h1; h += kRotRows) {
+                float x[kRotRows][2];
+#pragma unroll
+                for (int r = 0; r < kRotRows; ++r) {
+                    if constexpr (EB == 2) {
+                        x[r][0] = __uint_as_float(word[r] << 16);
+                        x[r][1] = __uint_as_float(word[r] & 0xffff0000u);
+                    } else {
+                        x[r][0] = __uint_as_float(word[r].x);
+                        x[r][1] = __uint_as_float(word[r].y);
                     }
-                    o16[ea] = (uint16_t)xa;
-                    o16[eb] = (uint16_t)xb;
-                } else {
-                    const float *f = reinterpret_cast<const float*>(in), x = f[ea], y = f[eb];
-                    float* o = reinterpret_cast<float*>(out);
-                    o[ea] = turn ? x * t.x - y * t.y : x;
-                    o[eb] = turn ? y * t.x + x * t.y : y;
+                    if (!INTERLEAVED) *reinterpret_cast<float2*>(&rows[w][r][2 * lane]) = make_float2(x[r][0], x[r][1]);
                 }
+                if (!INTERLEAVED) {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                }
+#pragma unroll
+                for (int r = 0; r < kRotRows; ++r) {
+                    float y[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const bool turn = 2 * lane + i < 2 * a.half;
+                        const float z = INTERLEAVED ? x[r][1 - i] : rows[w][r][partner[i]];
+                        y[i] = turn ? x[r][i] * c[i] + z * s[i] : x[r][i];
+                    }
+                    if (h + r < h1) {
+                        Word out;
+                        if constexpr (EB == 2) {
+                            out = bf16_pair(y[0], y[1]);
+                            // what is copied is copied bit by bit
+                            const uint32_t keep = (2 * lane < 2 * a.half ? 0u : 0xffffu) | (2 * lane + 1 < 2 * a.half ? 0u : 0xffff0000u);
+                            out = (out & ~keep) | (word[r] & keep);
+                        } else {
+                            out = make_uint2(__float_as_uint(y[0]), __float_as_uint(y[1]));
+                        }
+                        *reinterpret_cast<Word*>(row_out(h + r) + 2 * EB * lane) = out;
+                    }
+                }
+                if (!INTERLEAVED) {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                }
+                if (h + kRotRows < h1) load(h + kRotRows);
             }
         }
     }
@@ -841,42 +882,53 @@ __global__ __launch_bounds__(kWeightThreads) void cache_weights_kernel(CacheAtte
 }
 
 // ------------------------------------------------------------------------------------------------
-// Eviction: which rows of a (layer, sequence, head) stay.  One block each: every wave takes a share of neighbouring rows.  The cut is found digit by digit (11, 11, 10 bits) in
-// the order-preserving images of the weights; every wave then counts what it keeps of its share and writes it behind the shares before, in order.
-// KEYS: up to KEYS * 1024 rows, whose images stay in registers: the weights are read once.  0: any number, read in each of the five passes.
+// Eviction: which rows of a (layer, sequence, head) stay.  The cut is found digit by digit (11, 11, 10 bits) in the order-preserving images of the weights; every wave has a share of
+// neighbouring rows, counts what it keeps of them and writes it behind the shares before, in order.  The images stay in registers (KEYS * 1024 rows a block), so that
+// the weights are read once; the time goes into the five passes over them (32768 rows: 3 us to load, 5 for images and the first digit, 2 for each other one, 5 to count and write).
 // Counters: four of each digit, taken by lane, since gathered weights crowd into few digits (half of the rows may have the same one) and lanes that
 // add to one counter queue for it.
+// SLICED: longer heads, by several blocks each in four launches.  Launch i < 3 counts the i-th digit, the last one writes; what lies between two launches are the counts of every
+// slice, from which each block finds the next digit of the cut, and in the end its place in the list, by itself.  (131072 rows, 8 heads: 32 us; one block a head that reads them five times: 144.)
 // ------------------------------------------------------------------------------------------------
 struct EvictArgs {
     const float* acc;
     const int32_t *cu_tok, *n_tok;
     int32_t B, n_kv, T_total, max_n, keep, sink, recent;
     int32_t *keep_idx, *n_keep;
+    // SLICED
+    int64_t row0;
+    int32_t launch;
+    uint32_t* counts;           // [row of this launch][slice][kEvictSliceWords]: counts of the three digits
 };
 constexpr int kEvictDigits = 2048, kEvictCopies = 4;
 
-template <int KEYS>
+template <int KEYS, bool SLICED>
 __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a) {
     __shared__ __align__(16) uint32_t hist[kEvictDigits * kEvictCopies];
-    __shared__ uint32_t slot[kBlockWaves], slot2[kBlockWaves], found[2];
+    __shared__ uint32_t slot[kBlockWaves], slot2[kBlockWaves], found[2], s_above, s_equal;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int64_t row = blockIdx.x;                            // (layer * B + b) * Hkv + h
+    const int64_t row = SLICED ? a.row0 + blockIdx.y : blockIdx.x;             // (layer * B + b) * Hkv + h
+    const int slice = SLICED ? blockIdx.x : 0;
     const int h = (int)(row % a.n_kv), b = (int)(row / a.n_kv % a.B);
     const int64_t layer = row / a.n_kv / a.B;
     int32_t first, rows;
     region(a.cu_tok, b, a.T_total, &first, &rows);
     const int32_t n = min(min(max(a.n_tok[row], 0), a.max_n), rows);
     int32_t* out = a.keep_idx + row * max(a.keep, 1);
-    if (tid == 0) a.n_keep[row] = min(n, a.keep);
+    if (tid == 0 && slice == 0 && (!SLICED || a.launch == 3)) a.n_keep[row] = min(n, a.keep);
+    constexpr int32_t kSlice = KEYS * kBlockThreads;
+    const int32_t begin = SLICED ? slice * kSlice : 0, end = SLICED ? min(n - begin, kSlice) + begin : n;
+    if (begin >= end) return;
     if (n <= a.keep) {
-        for (int32_t j = tid; j < n; j += kBlockThreads) out[j] = j;
+        if (!SLICED || a.launch == 3)
+            for (int32_t j = begin + tid; j < end; j += kBlockThreads) out[j] = j;
         return;
     }
     if (a.keep == 0) return;
     const float* acc = a.acc + (layer * a.n_kv + h) * (int64_t)a.T_total + first;
-    const int32_t share = (n + kBlockThreads - 1) / kBlockThreads * 64, s0 = min(n, w * share), s1 = min(n, s0 + share);
+    const int32_t share = (end - begin + kBlockThreads - 1) / kBlockThreads * 64, s0 = min(end, begin + w * share), s1 = min(end, s0 + share);
     const int copy = lane & (kEvictCopies - 1);
-    // the images: rows that stay whatever they weigh above all others, lanes without a row below them (with NaN, which `in` tells apart)
+    // the images: rows that stay whatever they weigh above all others, lanes without a row below them (where NaN is, too)
     auto image = [&](int32_t j0 /* of the wave's first lane */, float f) -> uint32_t {
         uint32_t key = score_key(f);
         if (j0 < a.sink || j0 + 64 > min(n - a.recent, s1)) {
@@ -885,40 +937,72 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
         }
         return key;
     };
-    uint32_t keys[KEYS ? KEYS : 1];
-    if constexpr (KEYS > 0) {
+    uint32_t keys[KEYS];
 #pragma unroll
-        for (int i = 0; i < KEYS; ++i) keys[i] = __float_as_uint(acc[min(s0 + i * 64 + lane, n - 1)]);   // a load under a condition would wait for the one before
-    }
+    for (int i = 0; i < KEYS; ++i) keys[i] = __float_as_uint(acc[min(s0 + i * 64 + lane, n - 1)]);   // a load under a condition would wait for the one before
     for (int i = tid; i < kEvictDigits; i += kBlockThreads) *reinterpret_cast<uint4*>(hist + 4 * i) = make_uint4(0, 0, 0, 0);
+    if (tid == 0) s_above = s_equal = 0;
     __syncthreads();
-    // f(i, first row, the lane's image) for the wave's rows, 64 at a time
+    // f(i) for the wave's groups of 64 rows
     auto each = [&](auto f) {
-        if constexpr (KEYS > 0) {
 #pragma unroll
-            for (int i = 0; i < KEYS; ++i)
-                if (s0 + i * 64 < s1) f(i, s0 + i * 64, keys[i]);
-        } else {
-            for (int32_t j0 = s0; j0 < s1; j0 += 64) f(0, j0, image(j0, acc[min(j0 + lane, n - 1)]));
-        }
+        for (int i = 0; i < KEYS; ++i)
+            if (s0 + i * 64 < s1) f(i);
     };
+    const int slices = (n + kSlice - 1) / kSlice;
+    uint32_t* counts = SLICED ? a.counts + (int64_t)blockIdx.y * gridDim.x * kEvictSliceWords : nullptr;
+    const uint32_t d0 = 2047 - 2 * tid;                       // digits from the largest down, two a thread
     uint32_t need = (uint32_t)a.keep, prefix = 0;
+    bool imaged = false;
+    // SLICED, between the launches: in the first slice's words the cut so far and what is still needed (of each digit, two words), in every slice's the rows above it in slices before
+    uint32_t *known = counts + 3 * kEvictDigits, *own = counts + (int64_t)slice * kEvictSliceWords + 3 * kEvictDigits + 4;
+    if (SLICED && a.launch >= 2) {
+        prefix = known[2 * (a.launch - 2)];
+        need = known[2 * (a.launch - 2) + 1];
+        if (tid == 0) s_above = *own;
+    }
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
+        if (SLICED && pass < a.launch - 1) continue;
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
         const uint32_t digits = pass == 2 ? 1024u : 2048u;
-        each([&](int i, int32_t j0, uint32_t key) {
-            if (KEYS > 0 && pass == 0) keys[i] = key = image(j0, __uint_as_float(key));
-            if (pass == 0 || (key >> (pass == 1 ? 21 : 10)) == prefix) atomicAdd(&hist[((key >> shift) & (digits - 1)) * kEvictCopies + copy], 1u);
-        });
-        __syncthreads();
-        // digits from the largest down, two a thread: the one in which the count reaches `need`
-        const uint32_t d0 = 2047 - 2 * tid;
-        uint4 *p0 = reinterpret_cast<uint4*>(hist + d0 * 4), *p1 = reinterpret_cast<uint4*>(hist + (d0 - 1) * 4);
-        const uint4 h0 = *p0, h1 = *p1;
-        *p0 = make_uint4(0, 0, 0, 0);                         // for the next pass
-        *p1 = make_uint4(0, 0, 0, 0);
-        const uint32_t c0 = h0.x + h0.y + h0.z + h0.w, c1 = h1.x + h1.y + h1.z + h1.w;
+        uint32_t c0 = 0, c1 = 0, before0 = 0, before1 = 0;    // counts of the thread's digits, and of them those in slices before
+        if (SLICED && pass < a.launch) {
+            constexpr int kAhead = 8;                         // slices on their way
+            const uint32_t* p = counts + pass * kEvictDigits + (d0 - 1);
+            for (int s = 0; s < slices; s += kAhead) {
+                uint2 v[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) v[i] = *reinterpret_cast<const uint2*>(p + (int64_t)min(s + i, slices - 1) * kEvictSliceWords);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (s + i < slices) {
+                        c0 += v[i].y;
+                        c1 += v[i].x;
+                        before0 += s + i < slice ? v[i].y : 0u;
+                        before1 += s + i < slice ? v[i].x : 0u;
+                    }
+            }
+        } else {
+            each([&](int i) {
+                if (!imaged) keys[i] = image(s0 + i * 64, __uint_as_float(keys[i]));
+                const uint32_t key = keys[i];
+                if (pass == 0 || (key >> (pass == 1 ? 21 : 10)) == prefix) atomicAdd(&hist[((key >> shift) & (digits - 1)) * kEvictCopies + copy], 1u);
+            });
+            imaged = true;
+            __syncthreads();
+            uint4 *p0 = reinterpret_cast<uint4*>(hist + d0 * 4), *p1 = reinterpret_cast<uint4*>(hist + (d0 - 1) * 4);
+            const uint4 h0 = *p0, h1 = *p1;
+            *p0 = make_uint4(0, 0, 0, 0);                     // for the next pass
+            *p1 = make_uint4(0, 0, 0, 0);
+            c0 = h0.x + h0.y + h0.z + h0.w;
+            c1 = h1.x + h1.y + h1.z + h1.w;
+            if (SLICED) {
+                *reinterpret_cast<uint2*>(counts + (int64_t)slice * kEvictSliceWords + pass * kEvictDigits + (d0 - 1)) = make_uint2(c1, c0);
+                return;
+            }
+        }
+        // the digit in which the count reaches `need`
         uint32_t total;
         const uint32_t upto = block_scan_u32(c0 + c1, slot, &total), before = upto - c0 - c1;
         if (before < need && need <= upto) {
@@ -927,68 +1011,71 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
             found[1] = need - before - (second ? c0 : 0);
         }
         __syncthreads();
+        if (SLICED) {
+            const uint32_t digit = found[0], mine = (d0 > digit ? before0 : 0u) + (d0 - 1 > digit ? before1 : 0u);
+            if (mine) atomicAdd(&s_above, mine);
+            if (pass == 2 && (d0 == digit || d0 - 1 == digit)) s_equal = d0 == digit ? before0 : before1;
+        }
         prefix = (prefix << (pass == 2 ? 10 : 11)) | found[0];
         need = found[1];
-    }
-    // every row whose image is above `prefix`, and the first `need` of those equal to it.  A lane's kept rows are bits of a word where its images are in registers.
-    uint32_t above = 0, equal = 0, kept_rows = 0, equal_rows = 0;
-    each([&](int i, int32_t j0, uint32_t key) {
-        if constexpr (KEYS > 0) {
-            kept_rows |= key > prefix ? 1u << i : 0u;
-            equal_rows |= key == prefix ? 1u << i : 0u;
-        } else {
-            above += (uint32_t)__popcll(__ballot(key > prefix));
-            equal += (uint32_t)__popcll(__ballot(key == prefix && j0 + lane < s1));
+        if (SLICED) {
+            __syncthreads();
+            if (tid == 0 && a.launch < 3) {
+                *own = s_above;
+                if (slice == 0) {
+                    known[2 * pass] = prefix;
+                    known[2 * pass + 1] = need;
+                }
+            }
         }
-    });
-    if constexpr (KEYS > 0) {
-        if (prefix == 0) equal_rows &= s0 + lane < s1 ? (2u << ((s1 - 1 - s0 - lane) >> 6)) - 1 : 0u;      // NaN: lanes without a row look the same
-        above = __builtin_amdgcn_readlane((int)wave_scan_u32((uint32_t)__popc(kept_rows)), 63);
-        equal = __builtin_amdgcn_readlane((int)wave_scan_u32((uint32_t)__popc(equal_rows)), 63);
     }
+    if (!imaged) each([&](int i) { keys[i] = image(s0 + i * 64, __uint_as_float(keys[i])); });
+    // every row whose image is above `prefix`, and the first `need` of those equal to it: bits of a word a lane
+    uint32_t kept_rows = 0, equal_rows = 0;
+    each([&](int i) {
+        kept_rows |= keys[i] > prefix ? 1u << i : 0u;
+        equal_rows |= keys[i] == prefix ? 1u << i : 0u;
+    });
+    if (prefix == 0) equal_rows &= s0 + lane < s1 ? (2u << ((s1 - 1 - s0 - lane) >> 6)) - 1 : 0u;       // NaN: lanes without a row look the same
+    const uint32_t above = __builtin_amdgcn_readlane((int)wave_scan_u32((uint32_t)__popc(kept_rows)), 63);
+    const uint32_t equal = __builtin_amdgcn_readlane((int)wave_scan_u32((uint32_t)__popc(equal_rows)), 63);
     if (lane == 0) {
         slot[w] = above;
         slot2[w] = equal;
     }
     __syncthreads();
-    uint32_t before = lane < w ? slot[lane] : 0u, eq_before = lane < w ? slot2[lane] : 0u;
+    uint32_t above_before = lane < w ? slot[lane] : 0u, eq_before = lane < w ? slot2[lane] : 0u;
 #pragma unroll
     for (int m = 1; m < kBlockWaves; m <<= 1) {
-        before += (uint32_t)__shfl_xor((int)before, m);
+        above_before += (uint32_t)__shfl_xor((int)above_before, m);
         eq_before += (uint32_t)__shfl_xor((int)eq_before, m);
     }
-    uint32_t at = __builtin_amdgcn_readfirstlane((int)before), eq = __builtin_amdgcn_readfirstlane((int)eq_before);
+    uint32_t at = __builtin_amdgcn_readfirstlane((int)above_before), eq = __builtin_amdgcn_readfirstlane((int)eq_before);
+    if (SLICED) {
+        at += s_above;
+        eq += s_equal;
+    }
     at += min(eq, need);
-    // of 64 rows, `be` are equal to the cut and `eq` such rows lie before them: those that are still wanted, the lowest rows
-    auto wanted = [&](unsigned long long be) {
-        const uint32_t many = (uint32_t)__popcll(be);
-        for (uint32_t k = need - eq; k < many && be; ++k) be &= ~(1ull << (63 - __builtin_clzll(be)));
-        eq += many;
-        return be;
-    };
-    if constexpr (KEYS > 0) {
-        if (eq < need && equal > 0) {
-            if (eq + equal <= need) {
-                kept_rows |= equal_rows;
-            } else {
+    if (eq < need && equal > 0) {
+        if (eq + equal <= need) {
+            kept_rows |= equal_rows;
+        } else {                                              // the lowest ones that are still wanted
 #pragma unroll 1
-                for (int i = 0; i < KEYS && eq < need; ++i) kept_rows |= (uint32_t)(wanted(__ballot((equal_rows >> i) & 1)) >> lane & 1) << i;
+            for (int i = 0; i < KEYS && eq < need; ++i) {
+                unsigned long long be = __ballot((equal_rows >> i) & 1);
+                const uint32_t many = (uint32_t)__popcll(be);
+                for (uint32_t k = need - eq; k < many && be; ++k) be &= ~(1ull << (63 - __builtin_clzll(be)));
+                eq += many;
+                kept_rows |= (uint32_t)(be >> lane & 1) << i;
             }
         }
+    }
 #pragma unroll
-        for (int i = 0; i < KEYS; ++i) {
-            const bool mine = (kept_rows >> i) & 1;
-            const unsigned long long kept = __ballot(mine);
-            if (mine) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(kept >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)kept, 0u))] = s0 + i * 64 + lane;
-            at += (uint32_t)__popcll(kept);
-        }
-    } else {
-        each([&](int, int32_t j0, uint32_t key) {
-            unsigned long long kept = __ballot(key > prefix);
-            if (eq < need) kept |= wanted(__ballot(key == prefix && j0 + lane < s1));
-            if ((kept >> lane) & 1) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(kept >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)kept, 0u))] = j0 + lane;
-            at += (uint32_t)__popcll(kept);
-        });
+    for (int i = 0; i < KEYS; ++i) {
+        const bool mine = (kept_rows >> i) & 1;
+        const unsigned long long kept = __ballot(mine);
+        if (mine) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(kept >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)kept, 0u))] = s0 + i * 64 + lane;
+        at += (uint32_t)__popcll(kept);
     }
 }
 
@@ -1137,7 +1224,7 @@ hipError_t launch_rotary(Ctx* c, int32_t n, const void* q, const void* k, const 
     const int EB = c->d.kv_dtype == SKV_BF16 ? 2 : 4;
     const bool vec = rot % 16 == 0;
     RotArgs a{(const char*)q, (const char*)k, (char*)q_out, (char*)k_out, pos, inv_freq, n, q ? c->d.n_q_heads : 0, k ? c->d.n_kv_heads : 0, rot / 2, 0, mscale};
-    const int heads = a.n_q + a.n_k, rows = vec ? (EB == 2 ? 8 : 4) : 1;
+    const int heads = a.n_q + a.n_k, rows = vec && EB == 2 ? 8 : 4;
     // Few tokens: as few heads a wave as one load takes, for a short chain.  Many: all heads of a token, so that its angles are formed once (32768 tokens of 40 bf16 heads: 110 us with
     // one wave a token, 115 with two, 136 with five).  Between: as many waves as the chip has places for, 32 a compute unit.
     int groups = (heads + rows - 1) / rows;
@@ -1232,11 +1319,31 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
 
 hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_total, const int32_t* cu_tok, const int32_t* n_tok, int32_t max_n, int32_t keep,
                               int32_t sink, int32_t recent, int32_t* keep_idx, int32_t* n_keep) {
-    const EvictArgs a{acc, cu_tok, n_tok, B, c->d.n_kv_heads, T_total, max_n, keep, sink, recent, keep_idx, n_keep};
-    const dim3 grid(c->d.n_layers * B * c->d.n_kv_heads), threads(kBlockThreads);
-    if (max_n <= 8 * kBlockThreads) hipLaunchKernelGGL(cache_evict_kernel<8>, grid, threads, 0, c->stream, a);
-    else if (max_n <= 32 * kBlockThreads) hipLaunchKernelGGL(cache_evict_kernel<32>, grid, threads, 0, c->stream, a);
-    else hipLaunchKernelGGL(cache_evict_kernel<0>, grid, threads, 0, c->stream, a);
+    EvictArgs a{acc, cu_tok, n_tok, B, c->d.n_kv_heads, T_total, max_n, keep, sink, recent, keep_idx, n_keep, 0, 0, c->evict_counts};
+    const int64_t heads = (int64_t)c->d.n_layers * B * c->d.n_kv_heads;
+    const dim3 grid((unsigned)heads), threads(kBlockThreads);
+    if (max_n <= 8 * kBlockThreads) {
+        hipLaunchKernelGGL((cache_evict_kernel<8, false>), grid, threads, 0, c->stream, a);
+    } else if (max_n <= kEvictSlice) {
+        hipLaunchKernelGGL((cache_evict_kernel<kEvictSlice / kBlockThreads, false>), grid, threads, 0, c->stream, a);
+    } else {
+        // short slices where all of them have room and a place on the chip at once, long ones otherwise, as many heads at a time as there is room for
+        auto go = [&](auto keys) {
+            constexpr int K = decltype(keys)::value;
+            const int slices = (int)(((int64_t)max_n + K * kBlockThreads - 1) / (K * kBlockThreads)), at_once = evict_slices(c->d) / slices;
+            for (a.row0 = 0; a.row0 < heads; a.row0 += at_once) {
+                const unsigned here = (unsigned)(heads - a.row0 < at_once ? heads - a.row0 : at_once);
+                for (a.launch = 0; a.launch < 4; ++a.launch) {
+                    hipLaunchKernelGGL((cache_evict_kernel<K, true>), dim3(slices, here), threads, 0, c->stream, a);
+                    const hipError_t e = hipGetLastError();
+                    if (e != hipSuccess) return e;
+                }
+            }
+            return hipSuccess;
+        };
+        const int64_t few = heads * (((int64_t)max_n + 8 * kBlockThreads - 1) / (8 * kBlockThreads));
+        return few <= evict_slices(c->d) && few <= c->n_cu ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, kEvictSlice / kBlockThreads>{});
+    }
     return hipGetLastError();
 }
 

@@ -93,6 +93,7 @@ struct Ctx {
     unsigned long long* ret_list;
     unsigned int* ret_count;
     int32_t *ret_cut, *ret_chunk;
+    unsigned int* evict_counts;  // [evict_slices][kEvictSliceWords] (null: max_tokens up to kEvictSlice)
     unsigned int* n_sent_host;   // S of the last segmentation in pinned host memory (host address; null: none)
     unsigned int* n_sent_host_dev;   // its device address
     int wait_limit;              // polling rounds before a waiting block gives up
@@ -177,6 +178,13 @@ hipError_t launch_merge_lse(Ctx* c, const float* out_a, const float* lse_a, cons
                             int32_t n_heads, float* out, float* lse);
 
 // rotary positions and the 8-bit cache (cache.hip)
+// eviction from long heads in slices: rows of one, its counts of three digits and what is known between the launches, and slices that the context has room for
+constexpr int kEvictSlice = 32768, kEvictSliceWords = 3 * 2048 + 16;
+inline int evict_slices(const skv_desc& d) {
+    if (d.max_tokens <= kEvictSlice) return 0;
+    const int longest = (int)(((int64_t)d.max_tokens + kEvictSlice - 1) / kEvictSlice);
+    return longest > kComputeUnits ? longest : kComputeUnits;
+}
 hipError_t launch_rotary(Ctx* c, int32_t n, const void* q, const void* k, const int32_t* pos, const double* inv_freq, int32_t rot, bool interleaved,
                          float mscale, void* q_out, void* k_out);
 hipError_t launch_cache_append(Ctx* c, int32_t layer, int32_t B, const void* k, const void* v, int32_t n_new, const int32_t* cu_new, int32_t max_new,

@@ -479,7 +479,8 @@ def test_attend_large_and_small_magnitudes(shift):
 # ---- evict and compact ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,keep,sink,recent", [(0, 4, 1, 1), (1, 1, 0, 0), (5, 5, 2, 2), (5, 0, 0, 0), (6, 5, 2, 3), (6, 5, 2, 2), (300, 77, 4, 30), (1024, 1023, 0, 0), (1025, 64, 0, 64),
-                                                (1025, 64, 64, 0), (4097, 1000, 3, 500), (20000, 4096, 4, 1000), (70001, 9, 0, 1)])
+                                                (1025, 64, 64, 0), (4097, 1000, 3, 500), (20000, 4096, 4, 1000), (70001, 9, 0, 1),
+                                                (70001, 40000, 5, 34000), (32769, 32768, 0, 0), (150000, 150, 0, 0)])
 @pytest.mark.parametrize("kind", ["spread", "ties", "special", "close"])
 def test_evict(n, keep, sink, recent, kind):
     rng = np.random.RandomState(n + keep)
@@ -506,6 +507,30 @@ def test_evict(n, keep, sink, recent, kind):
                 got = idx[l, b, h].cpu().numpy()
                 assert int(n_keep[l, b, h]) == len(want)
                 assert np.array_equal(got[: len(want)], want) and np.all(got[len(want):] == -3), (l, b, h)
+
+
+@pytest.mark.parametrize("kind", ["spread", "ties"])
+def test_evict_of_more_long_heads_than_have_room_at_once(kind):
+    """100 heads of up to 40000 rows: their slices are counted in groups of heads; some heads are short, empty or hold less than may stay."""
+    rng = np.random.RandomState(5)
+    L, H, B, keep, sink, recent = 10, 2, 5, 3000, 2, 100
+    n = np.array([40000, 33000, 0, 2500, 9000])
+    cu = np.concatenate([[0], np.cumsum(n + 1)])
+    acc = rng.standard_normal((L, H, cu[-1])).astype(np.float32)
+    if kind == "ties":
+        acc = np.round(acc * 2)
+    n_tok = np.broadcast_to(n[None, :, None], (L, B, H)).copy()
+    n_tok[3, 0, 1] = 39990
+    ctx = context(L=L, H=H)
+    idx = torch.full((L, B, H, keep), -3, dtype=torch.int32, device=DEV)
+    n_keep = torch.full((L, B, H), -3, dtype=torch.int32, device=DEV)
+    ctx.cache_evict(B, torch.from_numpy(acc).to(DEV), int(cu[-1]), i32(cu), i32(n_tok), 180000, keep, sink, recent, idx, n_keep)
+    idx, n_keep = idx.cpu().numpy(), n_keep.cpu().numpy()
+    for l in range(L):
+        for b in range(B):
+            for h in range(H):
+                want = R.evict(acc[l, h, cu[b]: cu[b] + n_tok[l, b, h]], keep, sink, recent)
+                assert n_keep[l, b, h] == len(want) and np.array_equal(idx[l, b, h, : len(want)], want) and np.all(idx[l, b, h, len(want):] == -3), (l, b, h)
 
 
 def test_evict_cuts_counts_to_the_pool():
