@@ -576,8 +576,8 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
         for (int i = 0; i < kEntries; ++i) {
             const int32_t e = tid + i * kThreads;
             if (e < a.chunk) {
-                l_ks[e] = e_ks[i] * kToLog2;
-                l_vs[e] = e_vs[i];
+                l_ks[e] = entry[i] >= 0 ? e_ks[i] * kToLog2 : 0.0f;           // of no row: nothing that was read in its place
+                l_vs[e] = entry[i] >= 0 ? e_vs[i] : 0.0f;
             }
         }
         __syncthreads();
@@ -1279,7 +1279,7 @@ int64_t cache_attend_work_bytes(const Ctx* c, int32_t B, int32_t max_n, bool wei
 hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, const void* K, const void* V, const float* ks, const float* vs, int32_t T_total,
                                int32_t block, const int32_t* cu_tok, const int32_t* n_tok, const int32_t* tok_idx, int32_t max_n, float* out, float* lse,
                                const float* acc, float* acc_out, float decay, void* work) {
-    const bool listed = tok_idx != nullptr, weights = acc_out != nullptr, wide = c->d.kv_dtype != SKV_BF16;
+    const bool listed = tok_idx != nullptr && max_n > 0, weights = acc_out != nullptr, wide = c->d.kv_dtype != SKV_BF16;
     const AttendPlan p = attend_plan(c, B, max_n, listed, weights);
     const int H = c->d.n_kv_heads, n_scales = T_total / block + B, pairs = B * H;
     const int64_t pool = (int64_t)layer * H * T_total, sc = (int64_t)layer * H * n_scales;

@@ -390,6 +390,28 @@ def test_attend_leaves_out_what_is_not_in_use():
     check_attend(ref, 1, q, n2, out, lse, idx)
 
 
+def test_attend_scales_of_blocks_not_in_use_leave_no_trace():
+    """NaN in the scales of every block without rows in use (memory that nothing was written to): lists of entries that are no rows, empty sequences, empty lists."""
+    rng, ref, dev, ctx, q = attend_case(8, (64, 100, 5), 2, 4, "bf16", 32)
+    n = np.array([[33, 0], [99, 64], [0, 0]])
+    for b in range(3):
+        for h in range(2):
+            used = -(-int(n[b, h]) // 32)
+            ref.scale[:, :, h, ref.slot(b, 0) + used: ref.slot(b + 1, 0) if b < 2 else ref.ns] = np.nan
+    dev = device_cache(ref)
+    acc_out = torch.zeros(ref.acc.shape, device=DEV)
+    out, lse = run_attend(ref, dev, ctx, 1, q, i32(n), 100, acc_out=acc_out)
+    check_attend(ref, 1, q, n, out, lse, acc_out=(np.zeros(ref.acc.shape), f64(acc_out)))
+    idx = np.full((3, 2, 40), -1, np.int32)
+    idx[0, 0, :20], idx[1, :, 5:15] = np.arange(20), np.arange(10)
+    n2 = np.array([[40, 40], [30, 40], [40, 0]])
+    out, lse = run_attend(ref, dev, ctx, 1, q, i32(n2), 40, idx=i32(idx))
+    check_attend(ref, 1, q, n2, out, lse, idx)
+    assert np.all(out[2] == 0.0) and np.all(np.isneginf(lse[2])) and np.all(out[0, 4:] == 0.0)
+    out, lse = run_attend(ref, dev, ctx, 1, q, i32(n2), 0, idx=i32(idx))
+    assert np.all(out == 0.0) and np.all(np.isneginf(lse))
+
+
 def test_attend_counts_and_offsets_are_cut_to_the_pool():
     rng, ref, dev, ctx, q = attend_case(6, (37, 100), 2, 4, "bf16", 32)
     full = np.array([[ref.cu[b + 1] - ref.cu[b]] * 2 for b in range(2)])
