@@ -320,7 +320,7 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
 // ------------------------------------------------------------------------------------------------
 constexpr int kCacheTile = 32, kCacheWaves = 4, kCacheStep = kCacheTile * kCacheWaves;
 constexpr int kListedChunk = 1024;     // entries of a list per block, at most
-constexpr int kJoinInside = 32;        // parts of a pair up to which the attention kernel joins them itself
+constexpr int kJoinInside = 16;        // parts of a pair up to which the attention kernel joins them itself (16: 8.6 us, 9.0 by a launch of its own; 32: 11.8 and 9.2)
 constexpr int kSharePairs = 1024;      // pairs up to which the blocks take equal shares
 constexpr int kStageTiles = 8;         // tiles whose scores a wave keeps in LDS
 
@@ -410,7 +410,8 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
         for (int i = 0; i < kEach; ++i) {
             const int p = tid * kEach + i;
             int32_t f, r;
-            u[i] = p < a.pairs ? (rows_in_use(a, p, false, &f, &r) + kCacheStep - 1) / kCacheStep : 0;
+            const int32_t m = rows_in_use(a, min(p, a.pairs - 1), false, &f, &r);
+            u[i] = p < a.pairs ? (m + kCacheStep - 1) / kCacheStep : 0;
             sum += u[i];
         }
         const int32_t upto = (int32_t)wave_scan_u32((uint32_t)sum);
@@ -426,6 +427,10 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
                 if (blockIdx.x == 0) a.units[p] = before;
             }
             before += u[i];
+        }
+        if (a.pairs == kSharePairs && tid == kThreads - 1) {
+            s_units[a.pairs] = before;
+            if (blockIdx.x == 0) a.units[a.pairs] = before;
         }
         __syncthreads();
         const int32_t all = s_units[a.pairs], n_blocks = min((int32_t)gridDim.x, all);
@@ -754,12 +759,12 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
     }
     __syncthreads();
     if (!s_last) return;
-    // Everything is asked for at once: the references (through LDS, for all) and the first kJoinFirst sums of the two dims of up to two heads that a thread adds up.
+    // Everything is asked for at once: the references (through LDS, for all) and the sums of the two dims of up to two heads that a thread adds up.
     float2* s_ml = reinterpret_cast<float2*>(smem);           // [parts][G], at most 8 * kJoinInside = the threads
-    constexpr int kJoinFirst = 16, kItems = 8 * (kHeadDim / 2) / kThreads;
+    constexpr int kItems = 8 * (kHeadDim / 2) / kThreads;
     const int64_t pi0 = (int64_t)pair * a.splits * G;
     const unsigned long long m_own = ld_agent64(a.ml + 2 * (pi0 + min(tid, G * parts - 1)));
-    unsigned long long v[kItems][kJoinFirst];
+    unsigned long long v[kItems][kJoinInside];
     auto sums = [&](int k) {                                  // of the thread's item k
         const int e = min(tid + k * kThreads, G * (kHeadDim / 2) - 1);
         return a.part + (pi0 + e / (kHeadDim / 2)) * kHeadDim + e % (kHeadDim / 2) * 2;
@@ -768,7 +773,7 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
     for (int k = 0; k < kItems; ++k)
         if (k * kThreads < G * (kHeadDim / 2)) {
 #pragma unroll
-            for (int i = 0; i < kJoinFirst; ++i) v[k][i] = ld_agent64(sums(k) + (int64_t)min(i, parts - 1) * G * kHeadDim);
+            for (int i = 0; i < kJoinInside; ++i) v[k][i] = ld_agent64(sums(k) + (int64_t)min(i, parts - 1) * G * kHeadDim);
         }
     if (tid < G * parts) s_ml[tid] = make_float2(lo_f(m_own), hi_f(m_own));
     __syncthreads();
@@ -787,9 +792,8 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
             s1 += f * hi_f(p);
         };
 #pragma unroll
-        for (int i = 0; i < kJoinFirst; ++i)
+        for (int i = 0; i < kJoinInside; ++i)
             if (i < parts) add(i, v[k][i]);
-        for (int i = kJoinFirst; i < parts; ++i) add(i, ld_agent64(sums(k) + (int64_t)i * G * kHeadDim));
         const int64_t qi = (int64_t)pair * G + qg;
         store_out(a, qi, d, s0, z, top0);
         store_out(a, qi, d + 1, s1, z, top0);
@@ -1172,7 +1176,9 @@ inline int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 inline int log2_of(int32_t n) { return 31 - __builtin_clz((unsigned)n); }
 
 // How skv_cache_attend deals its work, and where the parts of the workspace begin.
-constexpr int kCacheRagged = 512;
+// Rows a block (of one a compute unit) from which a batch is dealt in equal shares: 16 sequences of 1024 to 4096 rows, 8 heads (2048) take 25.4 us by chunks and 26.2 in shares, of 2048 to
+// 8192 rows 41 and 35; 64 sequences of up to 1024 rows (2048) 24 and 35, up to 4096 76 and 77, up to 16384 254 and 221.  And rows a chunk of a batch that is dealt in those, at least.
+constexpr int kCacheShared = 2048, kCacheRagged = 512;
 struct AttendPlan {
     int deal;
     int32_t chunk, splits, blocks;         // kShare: blocks of the launch
@@ -1181,20 +1187,20 @@ struct AttendPlan {
 AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool weights) {
     AttendPlan p;
     const int64_t pairs = (int64_t)B * c->d.n_kv_heads, heads = pairs * c->G, rows = pairs * max_n;
-    const int pieces = c->d.kv_dtype == SKV_BF16 ? 1 : 3;
-    const int64_t most = (int64_t)c->n_cu * cache_places(pieces, kGrid, weights);        // blocks that the chip holds at once
-    int64_t chunk = round_up((rows + most - 1) / most, kCacheStep);
+    // One block a compute unit: with more a block's beginning and end (queries, counts, joining its waves) are paid more often than its waits are hidden (8 heads x 16384 rows
+    // 13.5 us with one, 13.8 with two, 14.9 with four; 64 lists of 2048 rows 13.9, 14.5, 17.6; 131072 rows 50, 50, 53).
+    int64_t chunk = round_up((rows + c->n_cu - 1) / c->n_cu, kCacheStep);
     if (chunk < kCacheStep) chunk = kCacheStep;
-    p.deal = listed ? kList : B > 1 && pairs <= kSharePairs && chunk > kCacheRagged / 2 ? kShare : kGrid;
+    p.deal = listed ? kList : B > 1 && pairs <= kSharePairs && chunk > kCacheShared ? kShare : kGrid;
     if (p.deal == kGrid && B > 1 && chunk > kCacheRagged) {               // sequences of unlike lengths: several rounds of shorter blocks
-        chunk = round_up((rows + 4 * most - 1) / (4 * most), kCacheStep);
+        chunk = round_up((rows + 4 * (int64_t)c->n_cu - 1) / (4 * (int64_t)c->n_cu), kCacheStep);
         if (chunk < kCacheRagged) chunk = kCacheRagged;
     }
     if (listed && chunk > kListedChunk) chunk = kListedChunk;
     p.chunk = (int32_t)chunk;
     p.splits = (int32_t)((max_n + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
-    p.blocks = cache_places(pieces, kShare, weights) * c->n_cu;
+    p.blocks = cache_places(c->d.kv_dtype == SKV_BF16 ? 1 : 3, kShare, weights) * c->n_cu;
     const int64_t slots = p.deal == kShare ? p.blocks + pairs : p.splits > 1 ? pairs * p.splits : 0;
     p.logit_rows = round_up(max_n, kCacheTile);
     p.ml = round_up(slots * c->G * kHeadDim * 4, 256);

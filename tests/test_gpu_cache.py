@@ -320,10 +320,11 @@ def test_attend_deals_long_batches_in_equal_shares(lengths, H, G, dtype, block, 
         assert np.array_equal(out, again[0]) and np.array_equal(lse, again[1])
 
 
-def test_attend_more_pairs_than_equal_shares_are_dealt_for():
-    lengths = tuple(int(x) for x in np.random.RandomState(0).randint(0, 200, 600))
+@pytest.mark.parametrize("B", [512, 513, 600])
+def test_attend_as_many_pairs_as_equal_shares_are_dealt_for_and_more(B):
+    lengths = tuple(int(x) for x in np.random.RandomState(0).randint(0, 200, B))
     rng, ref, dev, _, q = attend_case(1, lengths, 2, 1, "bf16", 32, L=1)
-    ctx = context(H=2, G=1, batch=600)
+    ctx = context(H=2, G=1, batch=B)
     n = np.array([[x, x // 2] for x in lengths])
     for max_n in (200, 3000):
         acc_out = torch.rand(ref.acc.shape, device=DEV)
