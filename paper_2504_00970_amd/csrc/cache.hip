@@ -216,12 +216,13 @@ __global__ __launch_bounds__(kRotWaves * kWave) void rotary_kernel(RotArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------
-// Append: one block per (sequence, head, K or V, scale block that takes new rows).  Bound by HBM for prompts (the rows in, half or a quarter of
+// Append: one block per (sequence, head, K or V, 32 to 128 rows of the scale blocks that take new rows).  Bound by HBM for prompts (the rows in, half or a quarter of
 // their bytes out), by the chain of its loads for single tokens.  The block's new rows stay in registers between the search for the
 // largest magnitude and the rounding.  Where rows are there already the scale can only grow; their codes are then rounded again.
 // ------------------------------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = kAppendThreads / 16;          // rows at a time: 16 lanes of 8 elements
+constexpr int kAppendSpan = 32;                           // rows of a launch block, at least (16384 tokens in blocks of 16: 25.0 us by 16 rows, 20.1 by 32, 20.5 by 64, 22.6 by 128)
 
 struct AppendArgs {
     const char *k, *v;
@@ -233,8 +234,10 @@ struct AppendArgs {
 
 template <int EB, int BLOCK>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs a) {
-    __shared__ uint32_t most[2][kAppendThreads / kWave];
-    constexpr int ITERS = BLOCK / kAppendRows, SHIFT = BLOCK == 16 ? 4 : BLOCK == 32 ? 5 : BLOCK == 64 ? 6 : 7;
+    constexpr int SPAN = BLOCK > kAppendSpan ? BLOCK : kAppendSpan, SUBS = SPAN / BLOCK;      // rows of a launch block, scale blocks among them
+    constexpr int ITERS = SPAN / kAppendRows, PER = BLOCK / kAppendRows, WAVES = kAppendThreads / kWave;
+    constexpr int SHIFT = BLOCK == 16 ? 4 : BLOCK == 32 ? 5 : BLOCK == 64 ? 6 : 7;
+    __shared__ uint32_t most[2][SUBS][WAVES];
     const int pair = blockIdx.x, b = pair / a.n_kv, h = pair % a.n_kv;
     const bool is_v = blockIdx.z != 0;
     const int tid = threadIdx.x, col = (tid & 15) * 8, r0 = tid >> 4;
@@ -249,9 +252,9 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
     float* scales = (is_v ? a.vs : a.ks) + (int64_t)h * a.n_scales + (first >> SHIFT) + b;
     uint8_t* pool = (is_v ? a.V : a.K) + ((int64_t)h * a.T_total + first) * kHeadDim + col;
     int buf = 0;
-    for (int32_t t = (held >> SHIFT) + blockIdx.y; t << SHIFT < held + m; t += gridDim.y, buf ^= 1) {
-        const int32_t base = t << SHIFT, lo = max(base, held), hi = min(base + BLOCK, held + m);     // the new rows of this block
-        const bool has_old = base < held;
+    for (int32_t t = (held >> SHIFT) + blockIdx.y * SUBS; t << SHIFT < held + m; t += gridDim.y * SUBS, buf ^= 1) {
+        const int32_t base = t << SHIFT, lo = max(base, held), hi = min(base + SPAN, held + m);     // the new rows of this block
+        const bool has_old = base < held;                     // in the first of its scale blocks
         const float old = has_old ? scales[t] : 0.0f;
         uint8_t* dst = pool + (int64_t)base * kHeadDim;
         uint4 x[ITERS * EB / 2];                              // rows that are not new: one that is, again (a load under a condition waits for those before it)
@@ -261,35 +264,46 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
 #pragma unroll
             for (int j = 0; j < EB / 2; ++j) x[i * (EB / 2) + j] = ld_stream(p + 16 * j);
         }
-        uint32_t big = 0;
+        uint32_t big[SUBS] = {};
 #pragma unroll
-        for (int i = 0; i < ITERS * EB / 2; ++i) {
-            float f[16 / EB];
-            unpack16<EB>(x[i], f);
+        for (int i = 0; i < ITERS; ++i) {
+            const int32_t row = base + r0 + i * kAppendRows;
+            uint32_t top = 0;
 #pragma unroll
-            for (int j = 0; j < 16 / EB; ++j) {
-                const uint32_t u = __float_as_uint(f[j]) & 0x7fffffffu;
-                big = max(big, u < kInfBits ? u : 0u);
+            for (int e = 0; e < EB / 2; ++e) {
+                float f[16 / EB];
+                unpack16<EB>(x[i * (EB / 2) + e], f);
+#pragma unroll
+                for (int j = 0; j < 16 / EB; ++j) {
+                    const uint32_t u = __float_as_uint(f[j]) & 0x7fffffffu;
+                    top = max(top, u < kInfBits ? u : 0u);
+                }
             }
+            big[i / PER] = max(big[i / PER], row >= lo && row < hi ? top : 0u);
         }
 #pragma unroll
-        for (int d = 32; d; d >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
-        if ((tid & 63) == 0) most[buf][tid >> 6] = big;
+        for (int s = 0; s < SUBS; ++s) {
+#pragma unroll
+            for (int d = 32; d; d >>= 1) big[s] = max(big[s], (uint32_t)__shfl_xor((int)big[s], d));
+            if ((tid & 63) == 0) most[buf][s][tid >> 6] = big[s];
+        }
         __syncthreads();
-        big = max(max(most[buf][0], most[buf][1]), max(most[buf][2], most[buf][3]));
-        const float s = fmaxf(old, scale_of(big));
-        if (has_old && s > old) {
-            const float f = old / s;
+        float scale[SUBS];
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) scale[s] = scale_of(max(max(most[buf][s][0], most[buf][s][1]), max(most[buf][s][2], most[buf][s][3])));
+        scale[0] = fmaxf(old, scale[0]);
+        if (has_old && scale[0] > old) {
+            const float f = old / scale[0];
             for (int32_t row = r0; row < held - base; row += kAppendRows) {
                 uint2* p = reinterpret_cast<uint2*>(dst + (int64_t)row * kHeadDim);
                 const uint2 w = *p;
                 *p = make_uint2(rescale(w.x, f), rescale(w.y, f));
             }
         }
-        const float inv = 1.0f / s;
 #pragma unroll
         for (int i = 0; i < ITERS; ++i) {
             const int32_t row = base + r0 + i * kAppendRows;
+            const float inv = 1.0f / scale[i / PER];
             float f[8];
 #pragma unroll
             for (int j = 0; j < EB / 2; ++j) unpack16<EB>(x[i * (EB / 2) + j], f + j * (16 / EB));
@@ -298,7 +312,9 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
             const unsigned long long w = codes_of(f[0], f[1], f[2], f[3]) | (unsigned long long)codes_of(f[4], f[5], f[6], f[7]) << 32;
             if (row >= lo && row < hi) __builtin_nontemporal_store(w, reinterpret_cast<unsigned long long*>(dst + (int64_t)(row - base) * kHeadDim));
         }
-        if (tid == 0) scales[t] = s;
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s)
+            if (tid == s && base + s * BLOCK < hi) scales[t + s] = scale[s];
         if (!is_v && a.acc)
             for (int32_t row = lo + tid; row < hi; row += kAppendThreads) a.acc[(int64_t)h * a.T_total + first + row] = 0.0f;
     }
@@ -889,7 +905,7 @@ __global__ __launch_bounds__(kWeightThreads) void cache_weights_kernel(CacheAtte
 // Eviction: which rows of a (layer, sequence, head) stay.  The cut is found digit by digit (11, 11, 10 bits) in the order-preserving images of the weights; every wave has a share of
 // neighbouring rows, counts what it keeps of them and writes it behind the shares before, in order.  The images stay in registers (KEYS * 1024 rows a block), so that
 // the weights are read once; the time goes into the five passes over them (32768 rows: 3 us to load, 5 for images and the first digit, 2 for each other one, 5 to count and write).
-// Counters: four of each digit, taken by lane, since gathered weights crowd into few digits (half of the rows may have the same one) and lanes that
+// Counters: two of each digit, taken by lane, since gathered weights crowd into few digits (half of the rows may have the same one) and lanes that
 // add to one counter queue for it.
 // SLICED: longer heads, by several blocks each in four launches.  Launch i < 3 counts the i-th digit, the last one writes; what lies between two launches are the counts of every
 // slice, from which each block finds the next digit of the cut, and in the end its place in the list, by itself.  (131072 rows, 8 heads: 32 us; one block a head that reads them five times: 144.)
@@ -904,13 +920,14 @@ struct EvictArgs {
     int32_t launch;
     uint32_t* counts;           // [row of this launch][slice][kEvictSliceWords]: counts of the three digits
 };
-constexpr int kEvictDigits = 2048, kEvictCopies = 4;
+constexpr int kEvictDigits = 2048, kEvictCopies = 2;
 
-template <int KEYS, bool SLICED>
-__global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a) {
+template <int THREADS, int KEYS, bool SLICED>
+__global__ __launch_bounds__(THREADS) void cache_evict_kernel(EvictArgs a) {
     __shared__ __align__(16) uint32_t hist[kEvictDigits * kEvictCopies];
-    __shared__ uint32_t slot[kBlockWaves], slot2[kBlockWaves], found[2], s_above, s_equal;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    constexpr int WAVES = THREADS / kWave, EACH = kEvictDigits / THREADS;      // digits a thread
+    __shared__ uint32_t slot[WAVES], slot2[WAVES], found[2], s_above, s_equal;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t row = SLICED ? a.row0 + blockIdx.y : blockIdx.x;             // (layer * B + b) * Hkv + h
     const int slice = SLICED ? blockIdx.x : 0;
     const int h = (int)(row % a.n_kv), b = (int)(row / a.n_kv % a.B);
@@ -920,17 +937,17 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
     const int32_t n = min(min(max(a.n_tok[row], 0), a.max_n), rows);
     int32_t* out = a.keep_idx + row * max(a.keep, 1);
     if (tid == 0 && slice == 0 && (!SLICED || a.launch == 3)) a.n_keep[row] = min(n, a.keep);
-    constexpr int32_t kSlice = KEYS * kBlockThreads;
+    constexpr int32_t kSlice = KEYS * THREADS;
     const int32_t begin = SLICED ? slice * kSlice : 0, end = SLICED ? min(n - begin, kSlice) + begin : n;
     if (begin >= end) return;
     if (n <= a.keep) {
         if (!SLICED || a.launch == 3)
-            for (int32_t j = begin + tid; j < end; j += kBlockThreads) out[j] = j;
+            for (int32_t j = begin + tid; j < end; j += THREADS) out[j] = j;
         return;
     }
     if (a.keep == 0) return;
     const float* acc = a.acc + (layer * a.n_kv + h) * (int64_t)a.T_total + first;
-    const int32_t share = (end - begin + kBlockThreads - 1) / kBlockThreads * 64, s0 = min(end, begin + w * share), s1 = min(end, s0 + share);
+    const int32_t share = (end - begin + THREADS - 1) / THREADS * 64, s0 = min(end, begin + w * share), s1 = min(end, s0 + share);
     const int copy = lane & (kEvictCopies - 1);
     // the images: rows that stay whatever they weigh above all others, lanes without a row below them (where NaN is, too)
     auto image = [&](int32_t j0 /* of the wave's first lane */, float f) -> uint32_t {
@@ -944,7 +961,7 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
     uint32_t keys[KEYS];
 #pragma unroll
     for (int i = 0; i < KEYS; ++i) keys[i] = __float_as_uint(acc[min(s0 + i * 64 + lane, n - 1)]);   // a load under a condition would wait for the one before
-    for (int i = tid; i < kEvictDigits; i += kBlockThreads) *reinterpret_cast<uint4*>(hist + 4 * i) = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < kEvictDigits * kEvictCopies / 4; i += THREADS) *reinterpret_cast<uint4*>(hist + 4 * i) = make_uint4(0, 0, 0, 0);
     if (tid == 0) s_above = s_equal = 0;
     __syncthreads();
     // f(i) for the wave's groups of 64 rows
@@ -955,7 +972,8 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
     };
     const int slices = (n + kSlice - 1) / kSlice;
     uint32_t* counts = SLICED ? a.counts + (int64_t)blockIdx.y * gridDim.x * kEvictSliceWords : nullptr;
-    const uint32_t d0 = 2047 - 2 * tid;                       // digits from the largest down, two a thread
+    const uint32_t d0 = kEvictDigits - EACH * (tid + 1);      // the thread's digits, d0 the lowest of them: the first threads have the largest
+    auto place = [](uint32_t d) { return d % EACH * THREADS + d / EACH; };          // counters of a thread's digits, so that the threads' lie side by side
     uint32_t need = (uint32_t)a.keep, prefix = 0;
     bool imaged = false;
     // SLICED, between the launches: in the first slice's words the cut so far and what is still needed (of each digit, two words), in every slice's the rows above it in slices before
@@ -970,55 +988,72 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
         if (SLICED && pass < a.launch - 1) continue;
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
         const uint32_t digits = pass == 2 ? 1024u : 2048u;
-        uint32_t c0 = 0, c1 = 0, before0 = 0, before1 = 0;    // counts of the thread's digits, and of them those in slices before
+        uint32_t c[EACH] = {}, before_slice[EACH] = {};       // counts of the thread's digits, and of them those in slices before
         if (SLICED && pass < a.launch) {
             constexpr int kAhead = 8;                         // slices on their way
-            const uint32_t* p = counts + pass * kEvictDigits + (d0 - 1);
+            const uint32_t* p = counts + pass * kEvictDigits + d0;
             for (int s = 0; s < slices; s += kAhead) {
-                uint2 v[kAhead];
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) v[i] = *reinterpret_cast<const uint2*>(p + (int64_t)min(s + i, slices - 1) * kEvictSliceWords);
+                uint32_t v[kAhead][EACH];
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i)
-                    if (s + i < slices) {
-                        c0 += v[i].y;
-                        c1 += v[i].x;
-                        before0 += s + i < slice ? v[i].y : 0u;
-                        before1 += s + i < slice ? v[i].x : 0u;
+#pragma unroll
+                    for (int k = 0; k < EACH; ++k) v[i][k] = p[(int64_t)min(s + i, slices - 1) * kEvictSliceWords + k];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                    for (int k = 0; k < EACH; ++k) {
+                        c[k] += s + i < slices ? v[i][k] : 0u;
+                        before_slice[k] += s + i < slices && s + i < slice ? v[i][k] : 0u;
                     }
             }
         } else {
             each([&](int i) {
                 if (!imaged) keys[i] = image(s0 + i * 64, __uint_as_float(keys[i]));
                 const uint32_t key = keys[i];
-                if (pass == 0 || (key >> (pass == 1 ? 21 : 10)) == prefix) atomicAdd(&hist[((key >> shift) & (digits - 1)) * kEvictCopies + copy], 1u);
+                const uint32_t d = (key >> shift) & (digits - 1);
+                if (pass == 0 || (key >> (pass == 1 ? 21 : 10)) == prefix) atomicAdd(&hist[place(d) * kEvictCopies + copy], 1u);
             });
             imaged = true;
             __syncthreads();
-            uint4 *p0 = reinterpret_cast<uint4*>(hist + d0 * 4), *p1 = reinterpret_cast<uint4*>(hist + (d0 - 1) * 4);
-            const uint4 h0 = *p0, h1 = *p1;
-            *p0 = make_uint4(0, 0, 0, 0);                     // for the next pass
-            *p1 = make_uint4(0, 0, 0, 0);
-            c0 = h0.x + h0.y + h0.z + h0.w;
-            c1 = h1.x + h1.y + h1.z + h1.w;
-            if (SLICED) {
-                *reinterpret_cast<uint2*>(counts + (int64_t)slice * kEvictSliceWords + pass * kEvictDigits + (d0 - 1)) = make_uint2(c1, c0);
-                return;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                uint2* p = reinterpret_cast<uint2*>(hist + place(d0 + k) * kEvictCopies);
+                const uint2 v = *p;
+                *p = make_uint2(0, 0);                        // for the next pass
+                c[k] = v.x + v.y;
+                if (SLICED) counts[(int64_t)slice * kEvictSliceWords + pass * kEvictDigits + d0 + k] = c[k];
             }
+            if (SLICED) return;
         }
-        // the digit in which the count reaches `need`
-        uint32_t total;
-        const uint32_t upto = block_scan_u32(c0 + c1, slot, &total), before = upto - c0 - c1;
-        if (before < need && need <= upto) {
-            const bool second = need > before + c0;
-            found[0] = d0 - (second ? 1 : 0);
-            found[1] = need - before - (second ? c0 : 0);
+        // the digit in which the count, from the largest one down, reaches `need`
+        uint32_t sum = 0;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) sum += c[k];
+        const uint32_t upto_wave = wave_scan_u32(sum);
+        if (lane == 63) slot[w] = upto_wave;
+        __syncthreads();
+        const uint32_t waves_to = wave_scan_u32(lane < WAVES ? slot[lane] : 0u);
+        uint32_t before = upto_wave - sum + (w ? (uint32_t)__builtin_amdgcn_readlane((int)waves_to, w - 1) : 0u);
+        if (before < need && need <= before + sum) {
+#pragma unroll
+            for (int k = EACH - 1; k >= 0; --k) {
+                if (before < need && need <= before + c[k]) {
+                    found[0] = d0 + k;
+                    found[1] = need - before;
+                }
+                before += c[k];
+            }
         }
         __syncthreads();
         if (SLICED) {
-            const uint32_t digit = found[0], mine = (d0 > digit ? before0 : 0u) + (d0 - 1 > digit ? before1 : 0u);
+            const uint32_t digit = found[0];
+            uint32_t mine = 0;
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                mine += d0 + k > digit ? before_slice[k] : 0u;
+                if (pass == 2 && d0 + k == digit) s_equal = before_slice[k];
+            }
             if (mine) atomicAdd(&s_above, mine);
-            if (pass == 2 && (d0 == digit || d0 - 1 == digit)) s_equal = d0 == digit ? before0 : before1;
         }
         prefix = (prefix << (pass == 2 ? 10 : 11)) | found[0];
         need = found[1];
@@ -1050,7 +1085,7 @@ __global__ __launch_bounds__(kBlockThreads) void cache_evict_kernel(EvictArgs a)
     __syncthreads();
     uint32_t above_before = lane < w ? slot[lane] : 0u, eq_before = lane < w ? slot2[lane] : 0u;
 #pragma unroll
-    for (int m = 1; m < kBlockWaves; m <<= 1) {
+    for (int m = 1; m < WAVES; m <<= 1) {
         above_before += (uint32_t)__shfl_xor((int)above_before, m);
         eq_before += (uint32_t)__shfl_xor((int)eq_before, m);
     }
@@ -1261,7 +1296,9 @@ hipError_t launch_cache_append(Ctx* c, int32_t layer, int32_t B, const void* k, 
     const AppendArgs a{(const char*)k, (const char*)v, (uint8_t*)K + pool * kHeadDim, (uint8_t*)V + pool * kHeadDim, ks + sc, vs + sc, acc ? acc + pool : nullptr,
                        cu_new, cu_tok, n_tok, n_new, max_new, T_total, n_scales, H};
     // pairs fastest: a token's heads lie side by side in the input, and the blocks that read them run at the same time
-    const int64_t blocks = ((int64_t)max_new + block - 2) / block + 1;
+    const int span = block > kAppendSpan ? block : kAppendSpan;
+    // a sequence's first scale block may hold up to block - 1 rows already
+    const int64_t blocks = ((int64_t)max_new + block - 1 + span - 1) / span;
     const dim3 grid(B * H, (unsigned)(blocks < 65535 ? blocks : 65535), 2);
     auto go = [&](auto eb) {
         constexpr int E = decltype(eb)::value;
@@ -1327,11 +1364,24 @@ hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_tot
                               int32_t sink, int32_t recent, int32_t* keep_idx, int32_t* n_keep) {
     EvictArgs a{acc, cu_tok, n_tok, B, c->d.n_kv_heads, T_total, max_n, keep, sink, recent, keep_idx, n_keep, 0, 0, c->evict_counts};
     const int64_t heads = (int64_t)c->d.n_layers * B * c->d.n_kv_heads;
-    const dim3 grid((unsigned)heads), threads(kBlockThreads);
-    if (max_n <= 8 * kBlockThreads) {
-        hipLaunchKernelGGL((cache_evict_kernel<8, false>), grid, threads, 0, c->stream, a);
+    const dim3 grid((unsigned)heads);
+    // as few threads a head as hold its images with eight each, then more images (a load of a row that is none costs as much as one of a row)
+    auto whole = [&](auto threads, auto keys) {
+        constexpr int N = decltype(threads)::value, K = decltype(keys)::value;
+        hipLaunchKernelGGL((cache_evict_kernel<N, K, false>), grid, dim3(N), 0, c->stream, a);
+    };
+    using std::integral_constant;
+    constexpr integral_constant<int, 8> k8{};
+    if (max_n <= 8 * 256) {
+        whole(integral_constant<int, 256>{}, k8);
+    } else if (max_n <= 8 * 512) {
+        whole(integral_constant<int, 512>{}, k8);
+    } else if (max_n <= 8 * 1024) {
+        whole(integral_constant<int, 1024>{}, k8);
+    } else if (max_n <= 16 * 1024) {
+        whole(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
     } else if (max_n <= kEvictSlice) {
-        hipLaunchKernelGGL((cache_evict_kernel<kEvictSlice / kBlockThreads, false>), grid, threads, 0, c->stream, a);
+        whole(integral_constant<int, 1024>{}, integral_constant<int, kEvictSlice / 1024>{});
     } else {
         // short slices where all of them have room and a place on the chip at once, long ones otherwise, as many heads at a time as there is room for
         auto go = [&](auto keys) {
@@ -1340,7 +1390,7 @@ hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_tot
             for (a.row0 = 0; a.row0 < heads; a.row0 += at_once) {
                 const unsigned here = (unsigned)(heads - a.row0 < at_once ? heads - a.row0 : at_once);
                 for (a.launch = 0; a.launch < 4; ++a.launch) {
-                    hipLaunchKernelGGL((cache_evict_kernel<K, true>), dim3(slices, here), threads, 0, c->stream, a);
+                    hipLaunchKernelGGL((cache_evict_kernel<kBlockThreads, K, true>), dim3(slices, here), dim3(kBlockThreads), 0, c->stream, a);
                     const hipError_t e = hipGetLastError();
                     if (e != hipSuccess) return e;
                 }
@@ -1348,7 +1398,7 @@ hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_tot
             return hipSuccess;
         };
         const int64_t few = heads * (((int64_t)max_n + 8 * kBlockThreads - 1) / (8 * kBlockThreads));
-        return few <= evict_slices(c->d) && few <= c->n_cu ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, kEvictSlice / kBlockThreads>{});
+        return few <= evict_slices(c->d) && few <= c->n_cu ? go(k8) : go(integral_constant<int, kEvictSlice / kBlockThreads>{});
     }
     return hipGetLastError();
 }
@@ -1358,10 +1408,11 @@ hipError_t launch_cache_compact(Ctx* c, int32_t B, const void* K, const void* V,
                                 float* vs_out, float* acc_out) {
     if (keep == 0) return hipSuccess;
     const int64_t heads = (int64_t)c->d.n_layers * B * c->d.n_kv_heads;
-    // other outputs: rows cut over blocks until there are four for every place on the chip (two blocks a compute unit), in groups of 128
+    // other outputs: rows cut over four blocks a compute unit, two of them at once, in groups of 128 (8 layers x 8 heads, 2048 of 4096 rows: 18.9 us with one, 17.7 with two, 18.5 with
+    // four, 21.7 with eight; 16 x 8 x 8192: 117, 108, 107, 105)
     int32_t span = keep;
     if (K != K_out) {
-        const int64_t cuts = (8 * (int64_t)c->n_cu + 2 * heads - 1) / (2 * heads);
+        const int64_t cuts = (4 * (int64_t)c->n_cu + 2 * heads - 1) / (2 * heads);
         span = (int32_t)round_up((keep + cuts - 1) / cuts, kCompactRows);
         if ((keep + span - 1) / span > 65535) span = (int32_t)round_up((keep + 65534) / 65535, kCompactRows);
     }
