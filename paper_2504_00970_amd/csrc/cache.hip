@@ -356,7 +356,7 @@ struct CacheAttendArgs {
     // from block + pair on, which no two pieces share since from one piece to the next the block or the pair goes up.
     float *out, *lse, *part, *ml, *lse2, *logits;
     int32_t* units;             // kShare: [pairs + 1] units before each pair, for the launch that joins
-    unsigned int* arrived;      // per pair, zero between launches; null: cache_join_kernel joins
+    unsigned int* arrived;      // per pair, zero between launches; null: cache_finish_kernel joins
 };
 
 // 8 bytes that are read once.
@@ -818,87 +818,115 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
     }
 }
 
-// Joins the partial results of the blocks of a (sequence, query head): a block for each quarter of the dims, the normaliser first, then the sums of 32 parts at a time.
-constexpr int kJoinThreads = 256, kJoinDims = 32, kJoinRows = kJoinThreads / (kJoinDims / 4);
-__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheAttendArgs a, int listed, int blocks /* kShare: of the attention; 0: not so */) {
-    __shared__ float s_top[kJoinThreads / kWave], s_z[kJoinThreads / kWave];
-    __shared__ __align__(16) float s_o[kJoinRows][kJoinDims];
-    const int64_t qi = blockIdx.x;
-    const int pair = (int)(qi / a.G), qg = (int)(qi % a.G), tid = threadIdx.x, r = tid / (kJoinDims / 4), d = tid % (kJoinDims / 4) * 4;
-    int splits;
-    int64_t slot;
-    if (blocks) {
+// What is left behind the attention launch, in one: blocks that join the partial results of a (sequence, query head), and blocks that add up the weights of 1024 rows of a
+// pair.  Neither waits for the other: the normalisers are as few numbers as there are parts, and whoever needs them takes them from there.
+constexpr int kFinishThreads = 256, kWeightRows = 4;          // rows a thread
+
+struct FinishArgs {
+    int32_t listed, share;      // share: blocks of the attention launch where it was kShare, else 0
+    int32_t joins;              // blocks of a pair that join: its heads (0: joined already)
+    const float* acc;
+    float *acc_out, decay;
+};
+
+// The slots of a pair's parts.
+__device__ __forceinline__ int parts_of(const CacheAttendArgs& a, const FinishArgs& f, int pair, int64_t* slot) {
+    if (f.share) {
         // a pair's first and last block: of n blocks, block k takes the units from floor(all k / n) on
-        const int64_t all = a.units[a.pairs], u0 = a.units[pair], u1 = a.units[pair + 1], nb = min((int64_t)blocks, all);
+        const int64_t all = a.units[a.pairs], u0 = a.units[pair], u1 = a.units[pair + 1], nb = min((int64_t)f.share, all);
         const int64_t k0 = u1 > u0 ? ((u0 + 1) * nb + all - 1) / all - 1 : 0, k1 = u1 > u0 ? (u1 * nb + all - 1) / all - 1 : -1;
-        splits = (int)(k1 - k0 + 1);
-        slot = k0 + pair;
-    } else {
-        int32_t first, rows;
-        splits = max(1, (rows_in_use(a, pair, listed != 0, &first, &rows) + a.chunk - 1) / a.chunk);
-        slot = (int64_t)pair * a.splits;
+        *slot = k0 + pair;
+        return (int)(k1 - k0 + 1);
     }
-    const float2* ml = reinterpret_cast<const float2*>(a.ml) + slot * a.G + qg;
-    const float* part = a.part + (slot * a.G + qg) * kHeadDim + blockIdx.y * kJoinDims + d;
+    int32_t first, rows;
+    *slot = (int64_t)pair * a.splits;
+    return max(1, (rows_in_use(a, pair, f.listed != 0, &first, &rows) + a.chunk - 1) / a.chunk);
+}
+
+// The largest reference and the normaliser relative to it (0 where that is -inf) of parts ml[0], ml[G], ..., by one wave.
+__device__ __forceinline__ float2 normaliser(const float2* ml, int parts, int G, int lane) {
     const float neg_inf = -__builtin_inff();
-    float top = neg_inf;
-    for (int i = tid; i < splits; i += kJoinThreads) top = fmaxf(top, ml[(int64_t)i * a.G].x);
+    float top = neg_inf, z = 0.0f;
+    for (int i = lane; i < parts; i += kWave) top = fmaxf(top, ml[(int64_t)i * G].x);
+#pragma unroll
     for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if ((tid & 63) == 0) s_top[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
     const float top0 = top == neg_inf ? 0.0f : top;
-    float z = 0.0f;
-    for (int i = tid; i < splits; i += kJoinThreads) {
-        const float2 v = ml[(int64_t)i * a.G];
+    for (int i = lane; i < parts; i += kWave) {
+        const float2 v = ml[(int64_t)i * G];
         z += __builtin_amdgcn_exp2f(v.x - top0) * v.y;
     }
+#pragma unroll
     for (int m = 32; m; m >>= 1) z += __shfl_xor(z, m);
-    if ((tid & 63) == 0) s_z[tid >> 6] = z;
-    __syncthreads();
-    z = (s_z[0] + s_z[1]) + (s_z[2] + s_z[3]);
+    return make_float2(top0, z);
+}
+
+// Eight parts of a head at a time.
+__device__ __forceinline__ void join_head(const CacheAttendArgs& a, const FinishArgs& f, int pair, int qg, float* s_o) {
+    constexpr int ROWS = kFinishThreads / (kHeadDim / 4);
+    const int tid = threadIdx.x, r = tid / (kHeadDim / 4), d = tid % (kHeadDim / 4) * 4;
+    int64_t slot;
+    const int parts = parts_of(a, f, pair, &slot);
+    const float2* ml = reinterpret_cast<const float2*>(a.ml) + slot * a.G + qg;
+    const float* part = a.part + (slot * a.G + qg) * kHeadDim + d;
+    const float2 n = normaliser(ml, parts, a.G, tid & 63);    // every wave for itself
     f32x4_t sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int i = r; i < splits; i += kJoinRows) sum += __builtin_amdgcn_exp2f(ml[(int64_t)i * a.G].x - top0) * *reinterpret_cast<const f32x4_t*>(part + (int64_t)i * a.G * kHeadDim);
-    *reinterpret_cast<f32x4_t*>(&s_o[r][d]) = sum;
+    for (int i = r; i < parts; i += ROWS) sum += __builtin_amdgcn_exp2f(ml[(int64_t)i * a.G].x - n.x) * *reinterpret_cast<const f32x4_t*>(part + (int64_t)i * a.G * kHeadDim);
+    *reinterpret_cast<f32x4_t*>(s_o + r * kHeadDim + d) = sum;
     __syncthreads();
-    if (tid < kJoinDims) {
+    if (tid < kHeadDim) {
         float v = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kJoinRows; ++i) v += s_o[i][tid];
-        store_out(a, qi, blockIdx.y * kJoinDims + tid, v, z, top0);
+        for (int i = 0; i < ROWS; ++i) v += s_o[i * kHeadDim + tid];
+        store_out(a, (int64_t)pair * a.G + qg, tid, v, n.y, n.x);
     }
 }
 
-// acc_out = decay * acc + the weights of the head's G queries, from the scores and the normalisers of the launches before.
-constexpr int kWeightThreads = 256, kWeightRows = 4;      // rows a thread
+// G: query heads of a KV head whose weights are added up: acc_out = decay * acc + their sum; 0: none.
 template <int G>
-__global__ __launch_bounds__(kWeightThreads) void cache_weights_kernel(CacheAttendArgs a, const float* acc, float* acc_out, float decay) {
-    const int pair = blockIdx.y, b = pair / a.n_kv, h = pair % a.n_kv;
-    int32_t first, rows;
-    region(a.cu_tok, b, a.T_total, &first, &rows);
-    const int32_t n = min(min(max(a.n_tok[pair], 0), a.max_n), rows);
-    const int32_t j = (blockIdx.x * kWeightThreads + threadIdx.x) * kWeightRows;
-    if (j >= n) return;
-    const int64_t at = (int64_t)h * a.T_total + first + j;
-    f32x4_t x[G];                                             // scores of 4 rows: 16-byte loads; the weights begin anywhere
-    float l2[G], old[kWeightRows], sum[kWeightRows];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-        x[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(a.logits + ((int64_t)pair * a.logit_rows + j / kCacheTile * kCacheTile) * G + g * kCacheTile + j % kCacheTile));
-        l2[g] = a.lse2[(int64_t)pair * G + g];
+__global__ __launch_bounds__(kFinishThreads) void cache_finish_kernel(CacheAttendArgs a, FinishArgs f) {
+    __shared__ __align__(16) float s_o[kFinishThreads * 4];
+    const int pair = blockIdx.y, tid = threadIdx.x;
+    if ((int)blockIdx.x < f.joins) {
+        join_head(a, f, pair, blockIdx.x, s_o);
+        return;
     }
+    if constexpr (G > 0) {
+        const int b = pair / a.n_kv, h = pair % a.n_kv;
+        int32_t first, rows;
+        region(a.cu_tok, b, a.T_total, &first, &rows);
+        const int32_t n = min(min(max(a.n_tok[pair], 0), a.max_n), rows), j0 = (int32_t)(blockIdx.x - f.joins) * kFinishThreads * kWeightRows;
+        if (j0 >= n) return;
+        const int32_t j = min(j0 + tid * kWeightRows, n - 1) / kWeightRows * kWeightRows;      // past the end: the last rows again, which are not stored
+        const int64_t at = (int64_t)h * a.T_total + first + j;
+        f32x4_t x[G];                                         // scores of 4 rows: 16-byte loads; the weights begin anywhere
+        float l2[G], sum[kWeightRows];
 #pragma unroll
-    for (int r = 0; r < kWeightRows; ++r) old[r] = acc && j + r < n ? acc[at + r] : 0.0f;
+        for (int g = 0; g < G; ++g)
+            x[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(a.logits + ((int64_t)pair * a.logit_rows + j / kCacheTile * kCacheTile) * G + g * kCacheTile + j % kCacheTile));
 #pragma unroll
-    for (int r = 0; r < kWeightRows; ++r) sum[r] = acc ? decay * old[r] : 0.0f;
+        for (int r = 0; r < kWeightRows; ++r) sum[r] = f.acc ? f.decay * f.acc[at + min(r, n - 1 - j)] : 0.0f;
+        if (f.joins) {
+            int64_t slot;
+            const int parts = parts_of(a, f, pair, &slot);
+            for (int g = tid >> 6; g < G; g += kFinishThreads / kWave) {
+                const float2 v = normaliser(reinterpret_cast<const float2*>(a.ml) + slot * G + g, parts, G, tid & 63);
+                if ((tid & 63) == 0) s_o[g] = v.y == 0.0f ? -__builtin_inff() : v.x + __builtin_log2f(v.y);
+            }
+            __syncthreads();
+        }
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+        for (int g = 0; g < G; ++g) l2[g] = f.joins ? s_o[g] : a.lse2[(int64_t)pair * G + g];
 #pragma unroll
-        for (int r = 0; r < kWeightRows; ++r) sum[r] += l2[g] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x[g][r] - l2[g]);
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-    for (int r = 0; r < kWeightRows; ++r)
-        if (j + r < n) acc_out[at + r] = sum[r];
+            for (int r = 0; r < kWeightRows; ++r) sum[r] += l2[g] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x[g][r] - l2[g]);
+        if (j0 + tid * kWeightRows < n) {
+#pragma unroll
+            for (int r = 0; r < kWeightRows; ++r)
+                if (j + r < n) f.acc_out[at + r] = sum[r];
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1211,8 +1239,9 @@ inline int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 inline int log2_of(int32_t n) { return 31 - __builtin_clz((unsigned)n); }
 
 // How skv_cache_attend deals its work, and where the parts of the workspace begin.
-// Rows a block (of one a compute unit) from which a batch is dealt in equal shares: 16 sequences of 1024 to 4096 rows, 8 heads (2048) take 25.4 us by chunks and 26.2 in shares, of 2048 to
-// 8192 rows 41 and 35; 64 sequences of up to 1024 rows (2048) 24 and 35, up to 4096 76 and 77, up to 16384 254 and 221.  And rows a chunk of a batch that is dealt in those, at least.
+// Rows a block (of one a compute unit) above which a batch is dealt in equal shares: of 16 sequences of 1024 to 4096 rows, 8 heads (2048) take 25.2 us by chunks and 25.1 in shares, of 2048
+// to 8192 rows 41 and 34; 64 sequences of up to 1024 rows (2048) 24 and 27, up to 16384 254 and 211.  With weights half as many: 16 x 4096 rows 37 by chunks and 31 in shares, 64 x
+// 1024 rows 35 and 31, 16 x 2048 (1024) 21 and 26.  And rows a chunk of a batch that is dealt in those, at least.
 constexpr int kCacheShared = 2048, kCacheRagged = 512;
 struct AttendPlan {
     int deal;
@@ -1226,7 +1255,7 @@ AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool
     // 13.5 us with one, 13.8 with two, 14.9 with four; 64 lists of 2048 rows 13.9, 14.5, 17.6; 131072 rows 50, 50, 53).
     int64_t chunk = round_up((rows + c->n_cu - 1) / c->n_cu, kCacheStep);
     if (chunk < kCacheStep) chunk = kCacheStep;
-    p.deal = listed ? kList : B > 1 && pairs <= kSharePairs && chunk > kCacheShared ? kShare : kGrid;
+    p.deal = listed ? kList : B > 1 && pairs <= kSharePairs && chunk > (weights ? kCacheShared / 2 : kCacheShared) ? kShare : kGrid;
     if (p.deal == kGrid && B > 1 && chunk > kCacheRagged) {               // sequences of unlike lengths: several rounds of shorter blocks
         chunk = round_up((rows + 4 * (int64_t)c->n_cu - 1) / (4 * (int64_t)c->n_cu), kCacheStep);
         if (chunk < kCacheRagged) chunk = kCacheRagged;
@@ -1339,25 +1368,19 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
     else if (weights) e = wide ? attend_launch<3, kGrid, true>(c, a, 0) : attend_launch<1, kGrid, true>(c, a, 0);
     else e = wide ? attend_launch<3, kGrid, false>(c, a, 0) : attend_launch<1, kGrid, false>(c, a, 0);
     if (e != hipSuccess) return e;
-    if (joined) {
-        hipLaunchKernelGGL(cache_join_kernel, dim3(pairs * c->G, kHeadDim / kJoinDims), dim3(kJoinThreads), 0, c->stream, a, listed ? 1 : 0,
-                           share ? p.blocks : 0);
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
+    const bool weigh = weights && max_n > 0;
+    if (!joined && !weigh) return hipSuccess;
+    const int per = kFinishThreads * kWeightRows;
+    const FinishArgs f{listed ? 1 : 0, share ? p.blocks : 0, joined ? c->G : 0, acc ? acc + pool : nullptr, weigh ? acc_out + pool : nullptr, decay};
+    const dim3 grid(f.joins + (weigh ? (max_n + per - 1) / per : 0), pairs), threads(kFinishThreads);
+    switch (weigh ? c->G : 0) {
+        case 0: hipLaunchKernelGGL(cache_finish_kernel<0>, grid, threads, 0, c->stream, a, f); break;
+        case 1: hipLaunchKernelGGL(cache_finish_kernel<1>, grid, threads, 0, c->stream, a, f); break;
+        case 2: hipLaunchKernelGGL(cache_finish_kernel<2>, grid, threads, 0, c->stream, a, f); break;
+        case 4: hipLaunchKernelGGL(cache_finish_kernel<4>, grid, threads, 0, c->stream, a, f); break;
+        default: hipLaunchKernelGGL(cache_finish_kernel<8>, grid, threads, 0, c->stream, a, f); break;
     }
-    if (weights && max_n > 0) {
-        const int per = kWeightThreads * kWeightRows;
-        const dim3 grid((max_n + per - 1) / per, pairs), block(kWeightThreads);
-        const float* from = acc ? acc + pool : nullptr;
-        switch (c->G) {
-            case 1: hipLaunchKernelGGL(cache_weights_kernel<1>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
-            case 2: hipLaunchKernelGGL(cache_weights_kernel<2>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
-            case 4: hipLaunchKernelGGL(cache_weights_kernel<4>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
-            default: hipLaunchKernelGGL(cache_weights_kernel<8>, grid, block, 0, c->stream, a, from, acc_out + pool, decay); break;
-        }
-        e = hipGetLastError();
-    }
-    return e;
+    return hipGetLastError();
 }
 
 hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_total, const int32_t* cu_tok, const int32_t* n_tok, int32_t max_n, int32_t keep,
