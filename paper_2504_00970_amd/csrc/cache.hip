@@ -60,7 +60,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 // Rotary positions: the pair (x, y) of frequency i becomes (x c - y s, y c + x s), c + i s = mscale * exp(i pos f_i).  Bound by HBM: rows in, rows
 // out.  An angle may be 10^6 and more, where 32 bits keep two digits of its fraction of a turn: it is formed and reduced in 64 bits, one frequency
 // a lane, once per wave.  A wave takes one token and some of its heads; a lane turns two 16-byte pieces of a row, whose partners lie in one
-// another (half layout) or in themselves (interleaved), so that a row may be turned where it lies.
+// another (half layout) or in themselves (interleaved), so that a row may be turned where it lies.  32768 tokens of 40 bf16 heads: 113 us, 5.9 TB/s.
 // ------------------------------------------------------------------------------------------------
 constexpr int kRotWaves = 4, kRotRows = 4;
 
@@ -219,6 +219,7 @@ __global__ __launch_bounds__(kRotWaves * kWave) void rotary_kernel(RotArgs a) {
 // Append: one block per (sequence, head, K or V, 32 to 128 rows of the scale blocks that take new rows).  Bound by HBM for prompts (the rows in, half or a quarter of
 // their bytes out), by the chain of its loads for single tokens.  The block's new rows stay in registers between the search for the
 // largest magnitude and the rounding.  Where rows are there already the scale can only grow; their codes are then rounded again.
+// 32768 tokens of 8 bf16 heads: 35 us, 5.8 TB/s; a token of 16 sequences 5.0.
 // ------------------------------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = kAppendThreads / 16;          // rows at a time: 16 lanes of 8 elements
@@ -331,8 +332,9 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
 // Eight of the sixteen columns hold queries, the others the same queries again, so that two pieces of 8 bits of the weights go through one instruction; with
 // a second one for the last piece a weight keeps 24 bits.  (With two pieces results were off by 2e-6 of themselves, with three by 5e-7; the time is the same.)  fp32
 // queries are split into three pieces that add up to them exactly.  Scores, maxima, sums and outputs are fp32.
-// A wave keeps a running reference per query (moved up only where a score exceeds it by 2^8: weights are then at most 256); the waves of a block and the blocks
-// of a (sequence, head) pair are joined by their references.
+// A wave keeps a running reference per query (scores are in powers of two; it is moved up only where one exceeds it by more than 8, so that weights are at most 256); the waves of a block
+// and the blocks of a (sequence, head) pair are joined by their references.
+// 131072 rows, 8 heads: 44 us, 6.1 TB/s, and the launch that joins.  With all of the arithmetic taken out it is the same: what counts is that the next tile is always on its way.
 // ------------------------------------------------------------------------------------------------
 constexpr int kCacheTile = 32, kCacheWaves = 4, kCacheStep = kCacheTile * kCacheWaves;
 constexpr int kListedChunk = 1024;     // entries of a list per block, at most
@@ -1152,7 +1154,7 @@ __global__ __launch_bounds__(THREADS) void cache_evict_kernel(EvictArgs a) {
 // A launch block takes `span` rows of one (layer, sequence, head, K or V) in ascending order, 128 at a time, eight lanes a row.  Where the outputs are the inputs `span` is all
 // of them: a group's rows lie at or behind the place they go to, those of later groups behind everything written, and every group is read before it is
 // written, so nothing is lost.  The rows of the next group and the list of the one behind are on their way while a group is written: a chain of three loads would
-// otherwise be waited for every 16 KB.
+// otherwise be waited for every 16 KB.  128 heads, 8192 of 16384 rows: 106 us, 5.2 TB/s; in place 116.
 // ------------------------------------------------------------------------------------------------
 constexpr int kCompactRows = 128;
 
