@@ -392,8 +392,8 @@ int skv_cache_attend(skv_ctx* ctx, int32_t layer, int32_t B, const void* q, cons
  * each head's own.
  * acc dev [L][Hkv][T_total];  n_tok dev [L][B][Hkv];  max_n >= the largest n_tok (rows behind are not looked at)
  * keep_idx dev [L][B][Hkv][max(keep, 1)] rows that stay, ascending, counted from the sequence's first (entries past n_keep are not written: with n_keep, a list that skv_gather
- *          and skv_cache_attend take, too);  n_keep dev [L][B][Hkv] = min(n, keep).  Asynchronous.
- * Errors: SKV_EINVAL (null / misaligned pointers, B < 1, T_total < 1, max_n < 0, keep < 0, sink < 0, recent < 0, sink + recent > keep), SKV_ECAPACITY (B > max_batch, T_total
+ *          and skv_cache_attend take, too);  n_keep dev [L][B][Hkv] = min(n, keep), not n_tok's own memory.  Asynchronous.
+ * Errors: SKV_EINVAL (null / misaligned pointers, n_keep == n_tok, B < 1, T_total < 1, max_n < 0, keep < 0, sink < 0, recent < 0, sink + recent > keep), SKV_ECAPACITY (B > max_batch, T_total
  * or max_n > max_tokens).
  *
  * skv_cache_compact: row j of a head becomes its row keep_idx[j], j < n_keep, for all layers, with its gathered weight (acc and acc_out, both or neither).  A block's new scale is the

@@ -707,6 +707,7 @@ int skv_cache_evict(skv_ctx* ctx, int32_t B, const float* acc, int32_t T_total, 
     if (!ctx) return SKV_EINVAL;
     if (B < 1 || T_total < 1 || max_n < 0 || keep < 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > keep) return SKV_EINVAL;
     if (bad_words(acc) || bad_ptr(cu_tok) || bad_words(n_tok) || bad_ptr(keep_idx) || bad_ptr(n_keep)) return SKV_EINVAL;
+    if (n_keep == n_tok) return SKV_EINVAL;                   // written while other blocks still read the counts
     if (B > ctx->c.d.max_batch || T_total > ctx->c.d.max_tokens || max_n > ctx->c.d.max_tokens) return SKV_ECAPACITY;
     const int rc = check_ctx(ctx);
     if (rc != SKV_OK) return rc;

@@ -82,23 +82,23 @@ class _Fake(ctypes.Structure):
 
 BUF = (ctypes.c_char * 64)()
 P = (ctypes.addressof(BUF) + 15) // 16 * 16             # an aligned address that nothing reads
+OTHER = P + 16
 
 GOOD = {
     "skv_rotary": dict(n=5, q=P, k=P, pos=P, inv_freq=P, rot=64, interleaved=0, mscale=1.0, q_out=P, k_out=P),
     "skv_cache_append": dict(layer=1, B=2, k=P, v=P, n_new=3, cu_new=P, max_new=3, cu_tok=P, n_tok=P, K=P, V=P, k_scale=P, v_scale=P, T_total=100, block=32, acc=P),
     "skv_cache_attend": dict(layer=1, B=2, q=P, K=P, V=P, k_scale=P, v_scale=P, T_total=100, block=32, cu_tok=P, n_tok=P, tok_idx=None, max_n=50, out=P, lse=P, acc=P,
                              acc_out=P, decay=0.5, work=P, work_bytes=1 << 30),
-    "skv_cache_evict": dict(B=2, acc=P, T_total=100, cu_tok=P, n_tok=P, max_n=50, keep=20, sink=4, recent=5, keep_idx=P, n_keep=P),
+    "skv_cache_evict": dict(B=2, acc=P, T_total=100, cu_tok=P, n_tok=P, max_n=50, keep=20, sink=4, recent=5, keep_idx=P, n_keep=OTHER),
     "skv_cache_compact": dict(B=2, K=P, V=P, k_scale=P, v_scale=P, acc=P, T_total=100, block=32, cu_tok=P, keep_idx=P, keep=20, n_keep=P, K_out=P, V_out=P, k_scale_out=P,
                               v_scale_out=P, acc_out=P),
 }
 INVALID, CAPACITY, PASSES = skv.SKV_EINVAL, skv.SKV_ECAPACITY, None
 NAN = float("nan")
-OTHER = P + 16
 CASES = [(name, {}, PASSES) for name in GOOD]
 for _name, _good in GOOD.items():
     for _arg in _good:
-        if _good[_arg] == P:
+        if _good[_arg] in (P, OTHER):
             optional = (_name, _arg) in (("skv_cache_append", "acc"), ("skv_cache_attend", "lse"), ("skv_cache_attend", "acc"))
             CASES.append((_name, {_arg: None}, PASSES if optional else INVALID))
             if _arg not in ("n_tok", "k_scale", "v_scale", "acc", "k_scale_out", "v_scale_out", "acc_out"):
@@ -122,7 +122,7 @@ CASES += [("skv_cache_attend", kw, want) for kw, want in [
 CASES += [("skv_cache_evict", kw, want) for kw, want in [
     (dict(B=0), INVALID), (dict(B=4), CAPACITY), (dict(T_total=0), INVALID), (dict(T_total=1001), CAPACITY), (dict(max_n=-1), INVALID), (dict(max_n=1001), CAPACITY),
     (dict(keep=-1, sink=0, recent=0), INVALID), (dict(sink=-1), INVALID), (dict(recent=-1), INVALID), (dict(sink=10, recent=11), INVALID), (dict(sink=10, recent=10), PASSES),
-    (dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1, keep=2 ** 31 - 1), INVALID)]]
+    (dict(n_keep=P), INVALID), (dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1, keep=2 ** 31 - 1), INVALID)]]
 CASES += [("skv_cache_compact", kw, want) for kw, want in [
     (dict(B=0), INVALID), (dict(B=4), CAPACITY), (dict(T_total=0), INVALID), (dict(T_total=1001), CAPACITY), (dict(block=31), INVALID), (dict(keep=-1), INVALID),
     (dict(acc=None, acc_out=None), PASSES), (dict(K_out=OTHER), INVALID), (dict(acc_out=OTHER), INVALID),
