@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(AppendArgs
 constexpr int kCacheTile = 32, kCacheWaves = 4, kCacheStep = kCacheTile * kCacheWaves;
 constexpr int kListedChunk = 1024;     // entries of a list per block, at most
 constexpr int kJoinInside = 16;        // parts of a pair up to which the attention kernel joins them itself (16: 8.6 us, 9.0 by a launch of its own; 32: 11.8 and 9.2)
-constexpr int kSharePairs = 1024;      // pairs up to which the blocks take equal shares
+constexpr int kSharePairs = 1024, kShareMost = 4096;      // pairs up to which the blocks take equal shares of long batches, and of skewed ones
 constexpr int kStageTiles = 8;         // tiles whose scores a wave keeps in LDS
 
 // How the rows are dealt to blocks.  kGrid: blocks of `chunk` rows of a (sequence, head) pair.  kList: the same of its list.  kShare: the rows of all pairs in a row, in units
@@ -422,33 +422,43 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
     int32_t unit = 0, unit_end = 0;
     if (DEAL == kShare) {
         __shared__ int32_t s_wave[kCacheWaves];
-        constexpr int kEach = kSharePairs / kThreads;
-        int32_t u[kEach], sum = 0;
+        constexpr int kEach = 4;
+        int32_t carried = 0;                                  // units before these pairs
+        int p0 = 0;
+        do {
+            int32_t u[kEach], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int p = tid * kEach + i;
-            int32_t f, r;
-            const int32_t m = rows_in_use(a, min(p, a.pairs - 1), false, &f, &r);
-            u[i] = p < a.pairs ? (m + kCacheStep - 1) / kCacheStep : 0;
-            sum += u[i];
-        }
-        const int32_t upto = (int32_t)wave_scan_u32((uint32_t)sum);
-        if (lane == 63) s_wave[w] = upto;
-        __syncthreads();
-        int32_t before = upto - sum;
-        for (int i = 0; i < w; ++i) before += s_wave[i];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int p = tid * kEach + i;
-            if (p <= a.pairs) {
-                s_units[p] = before;
-                if (blockIdx.x == 0) a.units[p] = before;
+            for (int i = 0; i < kEach; ++i) {
+                const int p = p0 + tid * kEach + i;
+                int32_t f, r;
+                const int32_t m = rows_in_use(a, min(p, a.pairs - 1), false, &f, &r);
+                u[i] = p < a.pairs ? (m + kCacheStep - 1) / kCacheStep : 0;
+                sum += u[i];
             }
-            before += u[i];
-        }
-        if (a.pairs == kSharePairs && tid == kThreads - 1) {
-            s_units[a.pairs] = before;
-            if (blockIdx.x == 0) a.units[a.pairs] = before;
+            const int32_t upto = (int32_t)wave_scan_u32((uint32_t)sum);
+            if (lane == 63) s_wave[w] = upto;
+            __syncthreads();
+            int32_t before = carried + upto - sum;
+#pragma unroll
+            for (int i = 0; i < kCacheWaves; ++i) {
+                before += i < w ? s_wave[i] : 0;
+                carried += s_wave[i];
+            }
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int p = p0 + tid * kEach + i;
+                before += u[i];
+                if (p < a.pairs) {
+                    s_units[p + 1] = before;
+                    if (blockIdx.x == 0) a.units[p + 1] = before;
+                }
+            }
+            p0 += kEach * kThreads;
+            if (p0 < a.pairs) __syncthreads();
+        } while (p0 < a.pairs);
+        if (tid == 0) {
+            s_units[0] = 0;
+            if (blockIdx.x == 0) a.units[0] = 0;
         }
         __syncthreads();
         const int32_t all = s_units[a.pairs], n_blocks = min((int32_t)gridDim.x, all);
@@ -1244,25 +1254,29 @@ inline int log2_of(int32_t n) { return 31 - __builtin_clz((unsigned)n); }
 // Rows a block (of one a compute unit) above which a batch is dealt in equal shares: of 16 sequences of 1024 to 4096 rows, 8 heads (2048) take 25.2 us by chunks and 25.1 in shares, of 2048
 // to 8192 rows 41 and 34; 64 sequences of up to 1024 rows (2048) 24 and 27, up to 16384 254 and 211.  With weights half as many: 16 x 4096 rows 37 by chunks and 31 in shares, 64 x
 // 1024 rows 35 and 31, 16 x 2048 (1024) 21 and 26.  And rows a chunk of a batch that is dealt in those, at least.
+// More pairs than kSharePairs take blocks of their own, which are then many and long enough (256 sequences of 1024 rows, 8 heads: 79 us by chunks, 101 in shares; 512 of up to 2048 198 and
+// 246), unless the longest sequence would keep its block busy for longer than the chip takes for all rows (255 of 1024 rows and one of 131072: 925 and 156).
 constexpr int kCacheShared = 2048, kCacheRagged = 512;
+constexpr int kGridChunk = 1 << 24;        // rows of a chunk whose bytes a 32-bit offset reaches
+bool skewed(const Ctx* c, int32_t max_n, int32_t T_total) { return (int64_t)max_n * c->n_cu > (int64_t)c->d.n_kv_heads * T_total; }
 struct AttendPlan {
     int deal;
     int32_t chunk, splits, blocks;         // kShare: blocks of the launch
     int64_t logit_rows, ml, lse2, units, logits, bytes;
 };
-AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool weights) {
+AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool weights, bool skewed) {
     AttendPlan p;
     const int64_t pairs = (int64_t)B * c->d.n_kv_heads, heads = pairs * c->G, rows = pairs * max_n;
     // One block a compute unit: with more a block's beginning and end (queries, counts, joining its waves) are paid more often than its waits are hidden (8 heads x 16384 rows
     // 13.5 us with one, 13.8 with two, 14.9 with four; 64 lists of 2048 rows 13.9, 14.5, 17.6; 131072 rows 50, 50, 53).
     int64_t chunk = round_up((rows + c->n_cu - 1) / c->n_cu, kCacheStep);
     if (chunk < kCacheStep) chunk = kCacheStep;
-    p.deal = listed ? kList : B > 1 && pairs <= kSharePairs && chunk > (weights ? kCacheShared / 2 : kCacheShared) ? kShare : kGrid;
+    p.deal = listed ? kList : B > 1 && (pairs <= kSharePairs || (skewed && pairs <= kShareMost)) && chunk > (weights ? kCacheShared / 2 : kCacheShared) ? kShare : kGrid;
     if (p.deal == kGrid && B > 1 && chunk > kCacheRagged) {               // sequences of unlike lengths: several rounds of shorter blocks
         chunk = round_up((rows + 4 * (int64_t)c->n_cu - 1) / (4 * (int64_t)c->n_cu), kCacheStep);
         if (chunk < kCacheRagged) chunk = kCacheRagged;
     }
-    if (listed && chunk > kListedChunk) chunk = kListedChunk;
+    if (chunk > (listed ? kListedChunk : kGridChunk)) chunk = listed ? kListedChunk : kGridChunk;
     p.chunk = (int32_t)chunk;
     p.splits = (int32_t)((max_n + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
@@ -1346,15 +1360,19 @@ hipError_t launch_cache_append(Ctx* c, int32_t layer, int32_t B, const void* k, 
 }
 
 int64_t cache_attend_work_bytes(const Ctx* c, int32_t B, int32_t max_n, bool weights) {
-    const int64_t a = attend_plan(c, B, max_n, false, weights).bytes, b = attend_plan(c, B, max_n, true, false).bytes;
-    return a > b ? a : b;
+    int64_t most = attend_plan(c, B, max_n, true, false, false).bytes;
+    for (const bool skewed : {false, true}) {
+        const int64_t bytes = attend_plan(c, B, max_n, false, weights, skewed).bytes;
+        if (bytes > most) most = bytes;
+    }
+    return most;
 }
 
 hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, const void* K, const void* V, const float* ks, const float* vs, int32_t T_total,
                                int32_t block, const int32_t* cu_tok, const int32_t* n_tok, const int32_t* tok_idx, int32_t max_n, float* out, float* lse,
                                const float* acc, float* acc_out, float decay, void* work) {
     const bool listed = tok_idx != nullptr && max_n > 0, weights = acc_out != nullptr, wide = c->d.kv_dtype != SKV_BF16;
-    const AttendPlan p = attend_plan(c, B, max_n, listed, weights);
+    const AttendPlan p = attend_plan(c, B, max_n, listed, weights, skewed(c, max_n, T_total));
     const int H = c->d.n_kv_heads, n_scales = T_total / block + B, pairs = B * H;
     const int64_t pool = (int64_t)layer * H * T_total, sc = (int64_t)layer * H * n_scales;
     const bool share = p.deal == kShare, joined = share || p.splits > kJoinInside;

@@ -333,6 +333,22 @@ def test_attend_as_many_pairs_as_equal_shares_are_dealt_for_and_more(B):
         check_attend(ref, 0, q, n, out, lse, acc=ref.acc, acc_out=(before, f64(acc_out)))
 
 
+@pytest.mark.parametrize("B,most,long", [(600, 900, 0), (600, 40, 20000), (2048, 20, 9000), (2049, 20, 9000)])
+def test_attend_of_more_pairs_alike_and_with_a_long_one_among_them(B, most, long):
+    """More pairs than those of long batches that always take shares: chunks of their own, or shares where one sequence has most of the rows, up to 4096 pairs."""
+    lengths = [int(x) for x in np.random.RandomState(1).randint(0, most, B)]
+    lengths[B - 2] = long or lengths[B - 2]
+    rng, ref, dev, _, q = attend_case(1, tuple(lengths), 2, 1, "bf16", 32, L=1)
+    ctx = context(H=2, G=1, batch=B)
+    n = np.array([[x, x // 2] for x in lengths])
+    acc_out = torch.rand(ref.acc.shape, device=DEV)
+    before = f64(acc_out)
+    out, lse = run_attend(ref, dev, ctx, 0, q, i32(n), max(lengths), acc=dev["acc"], acc_out=acc_out)
+    check_attend(ref, 0, q, n, out, lse, acc=ref.acc, acc_out=(before, f64(acc_out)))
+    two, lse2 = run_attend(ref, dev, ctx, 0, q, i32(n), max(lengths))
+    check_attend(ref, 0, q, n, two, lse2)
+
+
 def test_attend_of_many_rows_of_one_sequence():
     """More parts than the attention launch joins itself, and scores of more tiles than a wave keeps."""
     rng, ref, dev, ctx, q = attend_case(3, (70001,), 1, 2, "bf16", 128, L=1)
@@ -762,6 +778,28 @@ def test_a_cache_beyond_32_bits_of_bytes():
     ctx.cache_compact(2, K, V, ks, vs, acc, T, block, cu, idx, 100, n_keep, K, V, ks, vs, acc)
     assert same_codes(K[0, :, first: first + 400].cpu().numpy(), part.codes[0, 0, :, :400]) and same_codes(V[0, :, first: first + 400].cpu().numpy(), part.codes[1, 0, :, :400])
     assert int(K[0, 0, :first].max()) == 0
+
+
+def test_attend_of_one_long_sequence_among_more_pairs_than_take_shares():
+    """Its rows lie in chunks that a 32-bit offset reaches.  All weights are alike, and two rows have values."""
+    B, H, rows, block = 2049, 2, (1 << 25) + 999, 128
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    T = rows + B - 1
+    ctx = skv.Context(skv.Desc(n_layers=1, n_q_heads=H, n_kv_heads=H, kv_dtype=skv.SKV_BF16, max_tokens=T, max_batch=B))
+    K, V = (torch.zeros(1, H, T, D, dtype=torch.uint8, device=DEV) for _ in range(2))
+    ks, vs = (torch.ones(1, H, T // block + B, device=DEV) for _ in range(2))
+    V[0, 1, rows - 3, 5] = V[0, 1, 12, 6] = 0x7e                                  # 448
+    cu = i32(np.concatenate([[0], rows + np.arange(B)]))
+    n_tok = torch.ones(B, H, dtype=torch.int32, device=DEV)
+    n_tok[0, 1] = rows
+    q, out = torch.randn(B, H, D, device=DEV).bfloat16(), torch.full((B, H, D), 7.0, device=DEV)
+    work = torch.empty(ctx.cache_attend_work_bytes(B, rows), dtype=torch.uint8, device=DEV)
+    ctx.cache_attend(0, B, q, K, V, ks, vs, T, block, cu, n_tok, None, rows, out, None, None, None, 1.0, work)
+    got, want = f64(out), np.zeros((B, H, D))
+    want[0, 1, 5:7] = 448.0 / rows
+    # a lane of a wave adds up its rows' weights of 1 one by one, exactly up to 2^24; then waves and parts
+    assert np.all(np.abs(got - want) <= 400 * EPS * want)
 
 
 def test_calls_follow_the_contexts_stream():
