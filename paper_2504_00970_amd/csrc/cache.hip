@@ -20,6 +20,7 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));      // beginning at any word
 
 constexpr uint32_t kInfBits = 0x7f800000u;
 
@@ -357,7 +358,7 @@ struct CacheAttendArgs {
     // Partial results by slots of G heads: part [slot][G][D] sums, ml [slot][G] (reference, normaliser).  A pair's slots lie side by side: from pair * splits on, or (kShare)
     // from block + pair on, which no two pieces share since from one piece to the next the block or the pair goes up.
     float *out, *lse, *part, *ml, *lse2, *logits;
-    int32_t* units;             // kShare: [pairs + 1] units before each pair, for the launch that joins
+    int32_t* ends;              // kShare: [pairs][2] the first and the last block of each pair that has rows, for the launch that joins
     unsigned int* arrived;      // per pair, zero between launches; null: cache_finish_kernel joins
 };
 
@@ -448,18 +449,12 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
             for (int i = 0; i < kEach; ++i) {
                 const int p = p0 + tid * kEach + i;
                 before += u[i];
-                if (p < a.pairs) {
-                    s_units[p + 1] = before;
-                    if (blockIdx.x == 0) a.units[p + 1] = before;
-                }
+                if (p < a.pairs) s_units[p + 1] = before;
             }
             p0 += kEach * kThreads;
             if (p0 < a.pairs) __syncthreads();
         } while (p0 < a.pairs);
-        if (tid == 0) {
-            s_units[0] = 0;
-            if (blockIdx.x == 0) a.units[0] = 0;
-        }
+        if (tid == 0) s_units[0] = 0;
         __syncthreads();
         const int32_t all = s_units[a.pairs], n_blocks = min((int32_t)gridDim.x, all);
         if ((int32_t)blockIdx.x >= n_blocks) return;
@@ -480,7 +475,11 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
     const int b = pair / a.n_kv, h = pair % a.n_kv;
     const int32_t begin = DEAL == kShare ? __builtin_amdgcn_readfirstlane(s_units[pair]) : 0, stop = DEAL == kShare ? min(unit_end, (int32_t)__builtin_amdgcn_readfirstlane(s_units[pair + 1])) : 0;
     const int32_t j0 = DEAL == kShare ? (unit - begin) * kCacheStep : (int32_t)blockIdx.x * a.chunk;
-    if (DEAL == kShare) slot = blockIdx.x + pair;
+    if (DEAL == kShare) {
+        slot = blockIdx.x + pair;
+        if (tid == 0 && unit == begin) a.ends[2 * pair] = blockIdx.x;
+        if (tid == 0 && unit_end >= s_units[pair + 1]) a.ends[2 * pair + 1] = blockIdx.x;
+    }
 
     // a list's entries are asked for first: rows and scales wait for them
     constexpr int kEntries = LISTED ? kListedChunk / kThreads : 1;
@@ -835,7 +834,7 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
 constexpr int kFinishThreads = 256, kWeightRows = 4;          // rows a thread
 
 struct FinishArgs {
-    int32_t listed, share;      // share: blocks of the attention launch where it was kShare, else 0
+    int32_t listed, share;      // whether the attention launch was kList, kShare
     int32_t joins;              // blocks of a pair that join: its heads (0: joined already)
     const float* acc;
     float *acc_out, decay;
@@ -843,27 +842,28 @@ struct FinishArgs {
 
 // The slots of a pair's parts.
 __device__ __forceinline__ int parts_of(const CacheAttendArgs& a, const FinishArgs& f, int pair, int64_t* slot) {
-    if (f.share) {
-        // a pair's first and last block: of n blocks, block k takes the units from floor(all k / n) on
-        const int64_t all = a.units[a.pairs], u0 = a.units[pair], u1 = a.units[pair + 1], nb = min((int64_t)f.share, all);
-        const int64_t k0 = u1 > u0 ? ((u0 + 1) * nb + all - 1) / all - 1 : 0, k1 = u1 > u0 ? (u1 * nb + all - 1) / all - 1 : -1;
-        *slot = k0 + pair;
-        return (int)(k1 - k0 + 1);
-    }
     int32_t first, rows;
+    const int32_t n = rows_in_use(a, pair, f.listed != 0, &first, &rows);
+    if (f.share) {
+        const int32_t k0 = a.ends[2 * pair], k1 = a.ends[2 * pair + 1];
+        *slot = n > 0 ? k0 + pair : 0;
+        return n > 0 ? k1 - k0 + 1 : 0;
+    }
     *slot = (int64_t)pair * a.splits;
-    return max(1, (rows_in_use(a, pair, f.listed != 0, &first, &rows) + a.chunk - 1) / a.chunk);
+    return max(1, (n + a.chunk - 1) / a.chunk);
 }
 
 // The largest reference and the normaliser relative to it (0 where that is -inf) of parts ml[0], ml[G], ..., by one wave.
 __device__ __forceinline__ float2 normaliser(const float2* ml, int parts, int G, int lane) {
     const float neg_inf = -__builtin_inff();
-    float top = neg_inf, z = 0.0f;
-    for (int i = lane; i < parts; i += kWave) top = fmaxf(top, ml[(int64_t)i * G].x);
+    const float2 own = lane < parts ? ml[(int64_t)lane * G] : make_float2(neg_inf, 0.0f);      // mostly all there are
+    float top = own.x;
+    for (int i = lane + kWave; i < parts; i += kWave) top = fmaxf(top, ml[(int64_t)i * G].x);
 #pragma unroll
     for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
     const float top0 = top == neg_inf ? 0.0f : top;
-    for (int i = lane; i < parts; i += kWave) {
+    float z = __builtin_amdgcn_exp2f(own.x - top0) * own.y;
+    for (int i = lane + kWave; i < parts; i += kWave) {
         const float2 v = ml[(int64_t)i * G];
         z += __builtin_amdgcn_exp2f(v.x - top0) * v.y;
     }
@@ -916,8 +916,18 @@ __global__ __launch_bounds__(kFinishThreads) void cache_finish_kernel(CacheAtten
 #pragma unroll
         for (int g = 0; g < G; ++g)
             x[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(a.logits + ((int64_t)pair * a.logit_rows + j / kCacheTile * kCacheTile) * G + g * kCacheTile + j % kCacheTile));
+        const bool whole = j + kWeightRows <= n;
+        f32x4_any weights = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (f.acc) {
+            if (whole) {
+                weights = *reinterpret_cast<const f32x4_any*>(f.acc + at);
+            } else {
 #pragma unroll
-        for (int r = 0; r < kWeightRows; ++r) sum[r] = f.acc ? f.decay * f.acc[at + min(r, n - 1 - j)] : 0.0f;
+                for (int r = 0; r < kWeightRows; ++r) weights[r] = f.acc[at + min(r, n - 1 - j)];
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kWeightRows; ++r) sum[r] = f.acc ? f.decay * weights[r] : 0.0f;
         if (f.joins) {
             int64_t slot;
             const int parts = parts_of(a, f, pair, &slot);
@@ -934,9 +944,13 @@ __global__ __launch_bounds__(kFinishThreads) void cache_finish_kernel(CacheAtten
 #pragma unroll
             for (int r = 0; r < kWeightRows; ++r) sum[r] += l2[g] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x[g][r] - l2[g]);
         if (j0 + tid * kWeightRows < n) {
+            if (whole) {
+                *reinterpret_cast<f32x4_any*>(f.acc_out + at) = f32x4_any{sum[0], sum[1], sum[2], sum[3]};
+            } else {
 #pragma unroll
-            for (int r = 0; r < kWeightRows; ++r)
-                if (j + r < n) f.acc_out[at + r] = sum[r];
+                for (int r = 0; r < kWeightRows; ++r)
+                    if (j + r < n) f.acc_out[at + r] = sum[r];
+            }
         }
     }
 }
@@ -1262,7 +1276,7 @@ bool skewed(const Ctx* c, int32_t max_n, int32_t T_total) { return (int64_t)max_
 struct AttendPlan {
     int deal;
     int32_t chunk, splits, blocks;         // kShare: blocks of the launch
-    int64_t logit_rows, ml, lse2, units, logits, bytes;
+    int64_t logit_rows, ml, lse2, ends, logits, bytes;
 };
 AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool weights, bool skewed) {
     AttendPlan p;
@@ -1285,8 +1299,8 @@ AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool
     p.logit_rows = round_up(max_n, kCacheTile);
     p.ml = round_up(slots * c->G * kHeadDim * 4, 256);
     p.lse2 = p.ml + round_up(slots * c->G * 8, 256);
-    p.units = p.lse2 + round_up(heads * 4, 256);
-    p.logits = p.units + round_up((pairs + 1) * 4, 256);
+    p.ends = p.lse2 + round_up(heads * 4, 256);
+    p.logits = p.ends + round_up(pairs * 8, 256);
     p.bytes = p.logits + (weights ? round_up(heads * p.logit_rows * 4, 256) : 0);
     return p;
 }
@@ -1379,7 +1393,7 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
     char* ws = static_cast<char*>(work);
     const CacheAttendArgs a{(const char*)q, (const uint8_t*)K + pool * kHeadDim, (const uint8_t*)V + pool * kHeadDim, ks + sc, vs + sc, cu_tok, n_tok, tok_idx,
                             max_n, T_total, n_scales, log2_of(block), H, c->G, pairs, p.chunk, p.splits, p.logit_rows, out, lse, (float*)ws, (float*)(ws + p.ml),
-                            weights ? (float*)(ws + p.lse2) : nullptr, (float*)(ws + p.logits), (int32_t*)(ws + p.units),
+                            weights ? (float*)(ws + p.lse2) : nullptr, (float*)(ws + p.logits), (int32_t*)(ws + p.ends),
                             !joined && p.splits > 1 ? c->att_counter : nullptr};
     hipError_t e;
     if (listed) e = wide ? attend_launch<3, kList, false>(c, a, 0) : attend_launch<1, kList, false>(c, a, 0);
@@ -1391,7 +1405,7 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
     const bool weigh = weights && max_n > 0;
     if (!joined && !weigh) return hipSuccess;
     const int per = kFinishThreads * kWeightRows;
-    const FinishArgs f{listed ? 1 : 0, share ? p.blocks : 0, joined ? c->G : 0, acc ? acc + pool : nullptr, weigh ? acc_out + pool : nullptr, decay};
+    const FinishArgs f{listed ? 1 : 0, share ? 1 : 0, joined ? c->G : 0, acc ? acc + pool : nullptr, weigh ? acc_out + pool : nullptr, decay};
     const dim3 grid(f.joins + (weigh ? (max_n + per - 1) / per : 0), pairs), threads(kFinishThreads);
     switch (weigh ? c->G : 0) {
         case 0: hipLaunchKernelGGL(cache_finish_kernel<0>, grid, threads, 0, c->stream, a, f); break;
