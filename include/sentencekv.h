@@ -378,7 +378,8 @@ int skv_cache_append(skv_ctx* ctx, int32_t layer, int32_t B, const void* k, cons
  * tok_idx  dev [B][Hkv][max_n] or NULL: rows, counted from the sequence's first; an entry that is none of its rows is skipped, one that comes twice counts twice
  * acc_out  dev [L][Hkv][T_total] or NULL: of every row in use, acc_out = decay * acc + the sum of its weights over the G query heads of its KV head (acc NULL: 0 for it).
  *          acc and acc_out may be the same.  Not with tok_idx.
- * work     dev scratch of at least skv_cache_attend_work_bytes(ctx, B, max_n, acc_out != NULL) bytes (caller-owned; nothing is kept in it between calls)
+ * work     dev scratch of at least skv_cache_attend_work_bytes(ctx, B, max_n, acc_out != NULL) bytes (caller-owned; nothing is kept in it between calls).  That number is no
+ *          smaller for a larger B or max_n, nor with weights: a buffer for the largest call does for all smaller ones
  * Asynchronous: one launch, and one more for acc_out or where the rows of a head lie in more than 16 parts or a batch is long.
  * Errors: SKV_EINVAL (null / misaligned pointers, layer, B < 1, T_total < 1, max_n < 0, block, acc_out with tok_idx, acc without acc_out, decay not within [0, 1],
  * work too small), SKV_ECAPACITY (B > max_batch, T_total or max_n > max_tokens).  skv_cache_attend_work_bytes returns -1 for arguments the call would reject. */

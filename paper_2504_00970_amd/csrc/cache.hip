@@ -1273,14 +1273,28 @@ inline int log2_of(int32_t n) { return 31 - __builtin_clz((unsigned)n); }
 constexpr int kCacheShared = 2048, kCacheRagged = 512;
 constexpr int kGridChunk = 1 << 24;        // rows of a chunk whose bytes a 32-bit offset reaches
 bool skewed(const Ctx* c, int32_t max_n, int32_t T_total) { return (int64_t)max_n * c->n_cu > (int64_t)c->d.n_kv_heads * T_total; }
+struct AttendLayout {
+    int64_t logit_rows, ml, lse2, ends, logits, bytes;
+};
+AttendLayout attend_layout(const Ctx* c, int64_t pairs, int64_t slots, int32_t max_n, bool weights) {
+    AttendLayout w;
+    const int64_t heads = pairs * c->G;
+    w.logit_rows = round_up(max_n, kCacheTile);
+    w.ml = round_up(slots * c->G * kHeadDim * 4, 256);
+    w.lse2 = w.ml + round_up(slots * c->G * 8, 256);
+    w.ends = w.lse2 + round_up(heads * 4, 256);
+    w.logits = w.ends + round_up(pairs * 8, 256);
+    w.bytes = w.logits + (weights ? round_up(heads * w.logit_rows * 4, 256) : 0);
+    return w;
+}
 struct AttendPlan {
     int deal;
     int32_t chunk, splits, blocks;         // kShare: blocks of the launch
-    int64_t logit_rows, ml, lse2, ends, logits, bytes;
+    AttendLayout work;
 };
 AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool weights, bool skewed) {
     AttendPlan p;
-    const int64_t pairs = (int64_t)B * c->d.n_kv_heads, heads = pairs * c->G, rows = pairs * max_n;
+    const int64_t pairs = (int64_t)B * c->d.n_kv_heads, rows = pairs * max_n;
     // One block a compute unit: with more a block's beginning and end (queries, counts, joining its waves) are paid more often than its waits are hidden (8 heads x 16384 rows
     // 13.5 us with one, 13.8 with two, 14.9 with four; 64 lists of 2048 rows 13.9, 14.5, 17.6; 131072 rows 50, 50, 53).
     int64_t chunk = round_up((rows + c->n_cu - 1) / c->n_cu, kCacheStep);
@@ -1295,13 +1309,7 @@ AttendPlan attend_plan(const Ctx* c, int32_t B, int32_t max_n, bool listed, bool
     p.splits = (int32_t)((max_n + chunk - 1) / chunk);
     if (p.splits < 1) p.splits = 1;
     p.blocks = cache_places(c->d.kv_dtype == SKV_BF16 ? 1 : 3, kShare, weights) * c->n_cu;
-    const int64_t slots = p.deal == kShare ? p.blocks + pairs : p.splits > 1 ? pairs * p.splits : 0;
-    p.logit_rows = round_up(max_n, kCacheTile);
-    p.ml = round_up(slots * c->G * kHeadDim * 4, 256);
-    p.lse2 = p.ml + round_up(slots * c->G * 8, 256);
-    p.ends = p.lse2 + round_up(heads * 4, 256);
-    p.logits = p.ends + round_up(pairs * 8, 256);
-    p.bytes = p.logits + (weights ? round_up(heads * p.logit_rows * 4, 256) : 0);
+    p.work = attend_layout(c, pairs, p.deal == kShare ? p.blocks + pairs : p.splits > 1 ? pairs * p.splits : 0, max_n, weights);
     return p;
 }
 
@@ -1373,13 +1381,15 @@ hipError_t launch_cache_append(Ctx* c, int32_t layer, int32_t B, const void* k, 
     return hipGetLastError();
 }
 
+// Enough for every plan of up to B sequences and max_n rows, and no less for more of either: plans do not grow steadily (chunks are rounded up, shares need fewer parts than
+// chunks, lists take chunks of their own), and a buffer made for a cache's largest length has to do for every length on the way there.  Parts: pairs * ceil(max_n / chunk) <=
+// pairs + rows / chunk.  A chunk has 128 rows at least, and as many as n_cu (B > 1: 4 n_cu) blocks would need, unless that is cut to kListedChunk or more.  Shares take fewer than 4 n_cu
+// blocks, and only where there are more than 1024 rows a compute unit.
 int64_t cache_attend_work_bytes(const Ctx* c, int32_t B, int32_t max_n, bool weights) {
-    int64_t most = attend_plan(c, B, max_n, true, false, false).bytes;
-    for (const bool skewed : {false, true}) {
-        const int64_t bytes = attend_plan(c, B, max_n, false, weights, skewed).bytes;
-        if (bytes > most) most = bytes;
-    }
-    return most;
+    const int64_t pairs = (int64_t)B * c->d.n_kv_heads, rows = pairs * max_n, dealt = (B > 1 ? 4 : 1) * (int64_t)c->n_cu;
+    int64_t parts = rows / kCacheStep < dealt ? rows / kCacheStep : dealt;
+    if (rows / kListedChunk > parts) parts = rows / kListedChunk;
+    return attend_layout(c, pairs, pairs + parts, max_n, weights).bytes;
 }
 
 hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, const void* K, const void* V, const float* ks, const float* vs, int32_t T_total,
@@ -1392,8 +1402,8 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
     const bool share = p.deal == kShare, joined = share || p.splits > kJoinInside;
     char* ws = static_cast<char*>(work);
     const CacheAttendArgs a{(const char*)q, (const uint8_t*)K + pool * kHeadDim, (const uint8_t*)V + pool * kHeadDim, ks + sc, vs + sc, cu_tok, n_tok, tok_idx,
-                            max_n, T_total, n_scales, log2_of(block), H, c->G, pairs, p.chunk, p.splits, p.logit_rows, out, lse, (float*)ws, (float*)(ws + p.ml),
-                            weights ? (float*)(ws + p.lse2) : nullptr, (float*)(ws + p.logits), (int32_t*)(ws + p.ends),
+                            max_n, T_total, n_scales, log2_of(block), H, c->G, pairs, p.chunk, p.splits, p.work.logit_rows, out, lse, (float*)ws,
+                            (float*)(ws + p.work.ml), weights ? (float*)(ws + p.work.lse2) : nullptr, (float*)(ws + p.work.logits), (int32_t*)(ws + p.work.ends),
                             !joined && p.splits > 1 ? c->att_counter : nullptr};
     hipError_t e;
     if (listed) e = wide ? attend_launch<3, kList, false>(c, a, 0) : attend_launch<1, kList, false>(c, a, 0);

@@ -162,6 +162,29 @@ def test_null_contexts_and_work_sizes():
     assert _call("skv_cache_attend", ctypes.addressof(f), dict(work_bytes=size(2, 50, 1) - 1)) == skv.SKV_EINVAL
 
 
+@pytest.mark.parametrize("heads,group,dtype", [(1, 1, skv.SKV_BF16), (8, 4, skv.SKV_BF16), (8, 8, skv.SKV_F32), (15, 2, skv.SKV_F32)])
+def test_work_for_a_large_call_does_for_smaller_ones(heads, group, dtype):
+    """The bytes never fall as sequences, rows or weights are added, and the call takes a buffer of a larger one's size."""
+    f = _fake()
+    f.d.n_kv_heads, f.d.n_q_heads, f.d.kv_dtype, f.d.max_tokens, f.d.max_batch, f.G = heads, heads * group, dtype, 1 << 20, 4096, group
+    size = lambda *a: binding._lib().skv_cache_attend_work_bytes(ctypes.addressof(f), *a)      # noqa: E731
+    rows = sorted({max(0, int(x)) for p in range(21) for x in (2 ** p - 1, 2 ** p, 2 ** p + 1, 1.3 * 2 ** p)} | set(range(3500, 5500, 20)) | {(1 << 20)})
+    rows = [n for n in rows if n <= 1 << 20]
+    before = None
+    for B in (1, 2, 3, 16, 17, 64, 128, 129, 512, 513, 1024, 1025, 4096):
+        now = [[size(B, n, w) for n in rows] for w in (0, 1)]
+        for by_rows in now:
+            assert all(a <= b for a, b in zip(by_rows, by_rows[1:]))
+        assert all(a <= b for a, b in zip(*now))
+        assert before is None or all(a <= b for x, y in zip(before, now) for a, b in zip(x, y))
+        before = now
+    if not torch.cuda.is_available():                       # a call that passes its checks
+        for n in (0, 1, 129, 4000, 4159):
+            kw = dict(layer=0, B=1, T_total=5000, max_n=n, work_bytes=size(1, 4160, 1))
+            assert _call("skv_cache_attend", ctypes.addressof(f), kw) == skv.SKV_EHIP
+            assert _call("skv_cache_attend", ctypes.addressof(f), dict(kw, work_bytes=size(1, n, 1) - 1)) == skv.SKV_EINVAL
+
+
 @pytest.mark.parametrize("through", ["native", "ctypes"])
 @pytest.mark.parametrize("name", sorted(GOOD))
 def test_python_calls_refuse_arguments_in_each_others_place(name, through):
