@@ -371,7 +371,7 @@ int skv_cache_append(skv_ctx* ctx, int32_t layer, int32_t B, const void* k, cons
 
 /* skv_cache_attend: Eq. 3 for one token per sequence over the cache of layer `layer`: over the rows in use (tok_idx NULL) or over listed ones, as skv_select
  * writes them.  out and lse as in skv_attend (they merge with others by skv_merge_lse): no row gives out = 0, lse = -inf.  A NaN logit or one of +inf gives NaN in out,
- * lse and acc_out; a logit of -inf weighs nothing.  Logits, maxima, weights, sums and the products with V are fp32 (queries and weights enter the products in pieces of 8 bits, three of them where they have 24).
+ * lse and acc_out; a logit of -inf weighs nothing (0 times its value).  Logits, maxima, weights, sums and the products with V are fp32 (queries and weights enter the products in pieces of 8 bits, three of them where they have 24).
  * Results repeat bit for bit.
  * q dev [B][Hq][D] kv_dtype;  out dev [B][Hq][D] fp32;  lse dev [B][Hq] or NULL
  * max_n    >= the largest n_tok (more are not read).  With tok_idx: n_tok counts the entries of a list

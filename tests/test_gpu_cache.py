@@ -515,6 +515,49 @@ def test_attend_large_and_small_magnitudes(shift):
             assert np.all(np.abs(lse[b, h * 4:(h + 1) * 4] - wl) <= d + 400 * EPS * l1)
 
 
+def weight_bound(l1, lse, rows):
+    """A weight's relative error, as in check_attend."""
+    return 2 * 388 * EPS * l1 + 8 * EPS * float(np.abs(lse).max()) + 8 * EPS + (rows / 32 + 300) * EPS
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [(40, 7), (900, 300)])
+def test_attend_logits_of_minus_infinity_weigh_nothing(dtype, lengths):
+    """A query with an infinite element over keys that are positive there: all of its logits are -inf (nothing is weighed, as without rows) or +inf (NaN); the other
+    queries are what they are without it.  NaN queries stay NaN wherever their bits are."""
+    rng, ref, dev, ctx, q = attend_case(12, lengths, 2, 4, dtype, 64)
+    ref.codes[0, 1, :, :, 4] = rng.randint(1, 0x7f, ref.codes[0, 1, :, :, 4].shape)
+    dev, n = device_cache(ref), np.array([[x, x - 1] for x in lengths])
+    plain = q.clone()
+    q[:, 1, 4], q[:, 6, 4], q[:, 5, 4] = -math.inf, math.inf, math.nan
+    if dtype == "f32":
+        q.view(torch.int32)[:, 5, 4] = 0x7f800001              # NaN by its last bit
+    acc_out = torch.rand(ref.acc.shape, device=DEV)
+    want_out, want_lse = run_attend(ref, dev, ctx, 1, plain, i32(n), max(lengths))
+    idx = np.broadcast_to(np.arange(max(lengths)), (2, 2, max(lengths))).copy()
+    listed = run_attend(ref, dev, ctx, 1, q, i32(n), max(lengths), idx=i32(idx))
+    shares = run_attend(ref, dev, ctx, 1, q, i32(n), 400000)
+    weighed = run_attend(ref, dev, ctx, 1, q, i32(n), max(lengths), acc=dev["acc"], acc_out=acc_out, decay=0.5)
+    for out, lse in (run_attend(ref, dev, ctx, 1, q, i32(n), max(lengths)), listed, shares, weighed):
+        assert np.all(out[:, 1] == 0.0) and np.all(np.isneginf(lse[:, 1]))
+        assert np.all(np.isnan(out[:, 5:7])) and np.all(np.isnan(lse[:, 5:7]))
+        for i in (0, 2, 3, 4, 7):
+            assert np.all(np.abs(lse[:, i] - want_lse[:, i]) <= 1e-5 * np.abs(want_lse[:, i]) + 1e-5)
+            assert np.all(np.isfinite(out[:, i]))
+    for b in range(2):
+        at = ref.cu[b] + np.arange(n[b, 0])
+        finite = f64(plain)[b, [0, 2, 3]]
+        K, V = (ref.rows(kv, 1, 0, b, np.arange(n[b, 0])) for kv in range(2))
+        want, wl, p, l1 = R.attend(finite, K, V)
+        w = weight_bound(l1, wl, n[b, 0])
+        size = np.stack([(p[g][:, None] * np.abs(V)).sum(0) for g in range(3)])
+        for out, _ in (listed, shares, weighed):
+            assert np.all(np.abs(out[b, [0, 2, 3]] - want) <= 2 * w * size + 1e-30)
+        got, sure = f64(acc_out)[1, 0, at], 0.5 * ref.acc[1, 0, at] + p.sum(0)
+        assert np.all(np.abs(got - sure) <= p.sum(0) * 2 * w + 4 * EPS * sure)
+        assert np.all(np.isnan(f64(acc_out)[1, 1, ref.cu[b] + np.arange(n[b, 1])]))
+
+
 # ---- evict and compact ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,keep,sink,recent", [(0, 4, 1, 1), (1, 1, 0, 0), (5, 5, 2, 2), (5, 0, 0, 0), (6, 5, 2, 3), (6, 5, 2, 2), (300, 77, 4, 30), (1024, 1023, 0, 0), (1025, 64, 0, 64),
