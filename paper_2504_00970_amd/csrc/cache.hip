@@ -357,7 +357,7 @@ struct CacheAttendArgs {
     int64_t logit_rows;         // rows of a pair in `logits`: [pair][tile][G][32]
     // Partial results by slots of G heads: part [slot][G][D] sums, ml [slot][G] (reference, normaliser).  A pair's slots lie side by side: from pair * splits on, or (kShare)
     // from block + pair on, which no two pieces share since from one piece to the next the block or the pair goes up.
-    float *out, *lse, *part, *ml, *lse2, *logits;
+    float *out, *lse, *part, *ml, *norm, *logits;      // norm [pair][G][2]: reference and 1 / normaliser of a query, for the weights
     int32_t* ends;              // kShare: [pairs][2] the first and the last block of each pair that has rows, for the launch that joins
     unsigned int* arrived;      // per pair, zero between launches; null: cache_finish_kernel joins
 };
@@ -397,12 +397,16 @@ __device__ __forceinline__ int32_t rows_in_use(const CacheAttendArgs& a, int pai
     return listed ? n : min(n, *rows);
 }
 
+// What a weight is multiplied with: 1 / z, 0 where nothing is weighed.  Reference and normaliser stay apart: in one number, top0 + log2(z), the rounding of a
+// reference of thousands would be a relative error of every weight of the query (a logit of 4200 in powers of two: 1e-4 of them).
+__device__ __forceinline__ float share_of(float z) { return z == 0.0f ? 0.0f : 1.0f / z; }
+
 __device__ __forceinline__ void store_out(const CacheAttendArgs& a, int64_t qi, int d, float sum, float z, float top0) {
     a.out[qi * kHeadDim + d] = z == 0.0f ? 0.0f : sum / z;
     if (d == 0) {
         const float l2 = z == 0.0f ? -__builtin_inff() : top0 + __builtin_log2f(z);
         if (a.lse) a.lse[qi] = l2 * 0.6931471805599453f;
-        if (a.lse2) a.lse2[qi] = l2;
+        if (a.norm) *reinterpret_cast<float2*>(a.norm + 2 * qi) = make_float2(top0, share_of(z));
     }
 }
 
@@ -912,7 +916,8 @@ __global__ __launch_bounds__(kFinishThreads) void cache_finish_kernel(CacheAtten
         const int32_t j = min(j0 + tid * kWeightRows, n - 1) / kWeightRows * kWeightRows;      // past the end: the last rows again, which are not stored
         const int64_t at = (int64_t)h * a.T_total + first + j;
         f32x4_t x[G];                                         // scores of 4 rows: 16-byte loads; the weights begin anywhere
-        float l2[G], sum[kWeightRows];
+        float2 norm[G];
+        float sum[kWeightRows];
 #pragma unroll
         for (int g = 0; g < G; ++g)
             x[g] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(a.logits + ((int64_t)pair * a.logit_rows + j / kCacheTile * kCacheTile) * G + g * kCacheTile + j % kCacheTile));
@@ -933,16 +938,16 @@ __global__ __launch_bounds__(kFinishThreads) void cache_finish_kernel(CacheAtten
             const int parts = parts_of(a, f, pair, &slot);
             for (int g = tid >> 6; g < G; g += kFinishThreads / kWave) {
                 const float2 v = normaliser(reinterpret_cast<const float2*>(a.ml) + slot * G + g, parts, G, tid & 63);
-                if ((tid & 63) == 0) s_o[g] = v.y == 0.0f ? -__builtin_inff() : v.x + __builtin_log2f(v.y);
+                if ((tid & 63) == 0) reinterpret_cast<float2*>(s_o)[g] = make_float2(v.x, share_of(v.y));
             }
             __syncthreads();
         }
 #pragma unroll
-        for (int g = 0; g < G; ++g) l2[g] = f.joins ? s_o[g] : a.lse2[(int64_t)pair * G + g];
+        for (int g = 0; g < G; ++g) norm[g] = f.joins ? reinterpret_cast<const float2*>(s_o)[g] : reinterpret_cast<const float2*>(a.norm)[(int64_t)pair * G + g];
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int r = 0; r < kWeightRows; ++r) sum[r] += l2[g] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(x[g][r] - l2[g]);
+            for (int r = 0; r < kWeightRows; ++r) sum[r] += __builtin_amdgcn_exp2f(x[g][r] - norm[g].x) * norm[g].y;
         if (j0 + tid * kWeightRows < n) {
             if (whole) {
                 *reinterpret_cast<f32x4_any*>(f.acc_out + at) = f32x4_any{sum[0], sum[1], sum[2], sum[3]};
@@ -1274,15 +1279,15 @@ constexpr int kCacheShared = 2048, kCacheRagged = 512;
 constexpr int kGridChunk = 1 << 24;        // rows of a chunk whose bytes a 32-bit offset reaches
 bool skewed(const Ctx* c, int32_t max_n, int32_t T_total) { return (int64_t)max_n * c->n_cu > (int64_t)c->d.n_kv_heads * T_total; }
 struct AttendLayout {
-    int64_t logit_rows, ml, lse2, ends, logits, bytes;
+    int64_t logit_rows, ml, norm, ends, logits, bytes;
 };
 AttendLayout attend_layout(const Ctx* c, int64_t pairs, int64_t slots, int32_t max_n, bool weights) {
     AttendLayout w;
     const int64_t heads = pairs * c->G;
     w.logit_rows = round_up(max_n, kCacheTile);
     w.ml = round_up(slots * c->G * kHeadDim * 4, 256);
-    w.lse2 = w.ml + round_up(slots * c->G * 8, 256);
-    w.ends = w.lse2 + round_up(heads * 4, 256);
+    w.norm = w.ml + round_up(slots * c->G * 8, 256);
+    w.ends = w.norm + round_up(heads * 8, 256);
     w.logits = w.ends + round_up(pairs * 8, 256);
     w.bytes = w.logits + (weights ? round_up(heads * w.logit_rows * 4, 256) : 0);
     return w;
@@ -1403,7 +1408,7 @@ hipError_t launch_cache_attend(Ctx* c, int32_t layer, int32_t B, const void* q, 
     char* ws = static_cast<char*>(work);
     const CacheAttendArgs a{(const char*)q, (const uint8_t*)K + pool * kHeadDim, (const uint8_t*)V + pool * kHeadDim, ks + sc, vs + sc, cu_tok, n_tok, tok_idx,
                             max_n, T_total, n_scales, log2_of(block), H, c->G, pairs, p.chunk, p.splits, p.work.logit_rows, out, lse, (float*)ws,
-                            (float*)(ws + p.work.ml), weights ? (float*)(ws + p.work.lse2) : nullptr, (float*)(ws + p.work.logits), (int32_t*)(ws + p.work.ends),
+                            (float*)(ws + p.work.ml), weights ? (float*)(ws + p.work.norm) : nullptr, (float*)(ws + p.work.logits), (int32_t*)(ws + p.work.ends),
                             !joined && p.splits > 1 ? c->att_counter : nullptr};
     hipError_t e;
     if (listed) e = wide ? attend_launch<3, kList, false>(c, a, 0) : attend_launch<1, kList, false>(c, a, 0);

@@ -558,6 +558,39 @@ def test_attend_logits_of_minus_infinity_weigh_nothing(dtype, lengths):
         assert np.all(np.isnan(f64(acc_out)[1, 1, ref.cu[b] + np.arange(n[b, 1])]))
 
 
+@pytest.mark.parametrize("size", [16.0, 64.0, 256.0])
+@pytest.mark.parametrize("lengths,max_n", [((5,), 5), ((700,), 700), ((70001,), 70001), ((5, 3001), 400000)])
+@pytest.mark.parametrize("G,dtype", [(1, "bf16"), (8, "f32")])
+def test_gathered_weights_of_equal_rows_are_equal_parts_whatever_their_logits(size, lengths, max_n, G, dtype):
+    """Rows alike have one logit, of 260 to 4200 in powers of two.  Every weight's power is then 1 and the normaliser the number of rows, exactly: a weight is off by
+    the rounding of one quotient and of the product with it, the sum of G of them by G - 1 more.  In one block, in parts that the attention launch joins, in parts joined behind it, in shares."""
+    ref = R.Cache(np.concatenate([[0], np.cumsum(lengths)]), 1, 1, 32)
+    ref.codes[...] = 0x38                                      # 1
+    dev, ctx = device_cache(ref), context(L=1, H=1, G=G, dtype=dtype)
+    q = torch.full((len(lengths), G, D), size, dtype=TYPES[dtype], device=DEV)
+    acc_out = torch.zeros(ref.acc.shape, device=DEV)
+    out, _ = run_attend(ref, dev, ctx, 0, q, i32([[n] for n in lengths]), max_n, acc_out=acc_out)
+    assert np.all(np.abs(out - 1.0) <= 4 * EPS)
+    got = f64(acc_out)[0, 0]
+    for b, n in enumerate(lengths):
+        assert np.all(np.abs(got[ref.cu[b]: ref.cu[b + 1]] - G / n) <= (G + 2) * EPS * G / n), (b, n)
+
+
+@pytest.mark.parametrize("max_n", [900, 400000])
+def test_gathered_weights_of_large_logits_add_up(max_n):
+    """Logits of up to 10^5: whatever the weights are, those of a query add up to 1, since the normaliser is the sum of the same powers.  Off by the roundings of that sum (a lane's rows, then
+    waves and parts), by those of exponents, which are at most 64 half steps where a power counts, and by the products' own."""
+    rng, ref, dev, ctx, q = attend_case(13, (900, 333), 2, 4, "f32", 16)
+    ref.scale[0] *= 2.0 ** 13
+    dev, n = device_cache(ref), np.array([[900, 800], [333, 1]])
+    acc_out = torch.zeros(ref.acc.shape, device=DEV)
+    run_attend(ref, dev, ctx, 1, q, i32(n), max_n, acc_out=acc_out)
+    for b in range(2):
+        for h in range(2):
+            total = f64(acc_out)[1, h, ref.cu[b]: ref.cu[b] + n[b, h]].sum()
+            assert abs(total - 4.0) <= 4.0 * (n[b, h] / 32 + 400) * EPS, (b, h, total)
+
+
 # ---- evict and compact ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,keep,sink,recent", [(0, 4, 1, 1), (1, 1, 0, 0), (5, 5, 2, 2), (5, 0, 0, 0), (6, 5, 2, 3), (6, 5, 2, 2), (300, 77, 4, 30), (1024, 1023, 0, 0), (1025, 64, 0, 64),
