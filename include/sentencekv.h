@@ -318,7 +318,7 @@ int skv_merge_lse(skv_ctx* ctx, int32_t n_heads, const float* out_a, const float
  * Rotary positions.  A head's first `rot` elements form rot / 2 pairs; pair i of a row at position p turns by the angle p * inv_freq[i]:
  *     (x, y) -> m * (x cos - y sin, y cos + x sin),   m = mscale
  * `interleaved` == 0: pair i is (i, i + rot / 2);  1: (2 i, 2 i + 1).  The elements from `rot` on are copied.  Angles are formed and reduced to a turn in 64 bits
- * (positions of 10^6 and more lose nothing), products are fp32, rounded once to kv_dtype.  Negated positions turn back: with m = 1 that is the inverse, with any m
+ * (positions of 10^6 and more lose nothing), their sines and cosines are within 3 units of the last place of fp32, products are fp32, rounded once to kv_dtype.  Negated positions turn back: with m = 1 that is the inverse, with any m
  * the transposed map (what a gradient goes through).
  *
  * skv_rotary_freqs fills a table of frequencies (host memory; the caller copies it to the device) and the factor m:

@@ -97,7 +97,9 @@ __global__ __launch_bounds__(kRotWaves * kWave) void rotary_kernel(RotArgs a) {
                 const float r = (float)(turns - rint(turns));
                 float s, c;
                 sincospif(2.0f * r, &s, &c);
-                table[w][lane] = make_float2(c * a.mscale, s * a.mscale);
+                // what r's 32 bits left out, up to 2^-26 turns: the first order of its rotation (the second one is below 2^-47)
+                const float rest = (float)(turns - rint(turns) - (double)r) * 6.283185307f;
+                table[w][lane] = make_float2((c - s * rest) * a.mscale, (s + c * rest) * a.mscale);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();

@@ -104,6 +104,27 @@ def test_rotary_of_many_tokens_takes_each_once():
     ctx.rotary(0, x, None, pos, freq, 64, False, 1.0, out, None)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [40, 64, 126, 128])
+def test_rotary_sines_near_half_a_turn(interleaved, rot):
+    """Angles next to odd multiples of pi, where the sine is small beside the angle: a fraction of a turn that was rounded to 32 bits would lose up to 9e-8 of it.  Rows of (1, 0) show
+    cosine and sine themselves.  Sines and cosines are within 2 units of the last place (4 half steps), the rest of the angle is added with one rounding; the 64-bit angle is
+    off by less than 2^-50 of 7 pi, below 2^-24 of the smallest sine."""
+    half = rot // 2
+    freq = math.pi * (1.0 + np.exp2(-np.linspace(4.0, 18.0, half)) * np.where(np.arange(half) % 2, -1.0, 1.0))
+    pos = np.array([1, -1, 3, 7, -5], np.int32)
+    x = torch.zeros(5, 2, D)
+    a = np.arange(half) * 2 if interleaved else np.arange(half)
+    b = a + (1 if interleaved else half)
+    x[:, :, a] = 1.0
+    ctx, out = context(H=1, G=2, dtype="f32"), torch.zeros(5, 2, D, device=DEV)
+    ctx.rotary(5, x.to(DEV), None, i32(pos), torch.from_numpy(freq).to(DEV), rot, interleaved, 1.0, out, None)
+    angle = pos[:, None].astype(np.float64) * freq[None]
+    for at, want in ((a, np.cos(angle)), (b, np.sin(angle))):
+        got = f64(out)[:, :, at]
+        assert np.all(np.abs(got - want[:, None]) <= 6 * EPS * np.abs(want[:, None])), (np.abs(got / want[:, None] - 1)).max()
+
+
 # ---- append ---------------------------------------------------------------------------------------------------------------
 
 def device_cache(ref):
