@@ -976,8 +976,8 @@ struct EvictArgs {
     const int32_t *cu_tok, *n_tok;
     int32_t B, n_kv, T_total, max_n, keep, sink, recent;
     int32_t *keep_idx, *n_keep;
+    int64_t row0;               // the first head of this launch
     // SLICED
-    int64_t row0;
     int32_t launch;
     uint32_t* counts;           // [row of this launch][slice][kEvictSliceWords]: counts of the three digits
 };
@@ -989,7 +989,7 @@ __global__ __launch_bounds__(THREADS) void cache_evict_kernel(EvictArgs a) {
     constexpr int WAVES = THREADS / kWave, EACH = kEvictDigits / THREADS;      // digits a thread
     __shared__ uint32_t slot[WAVES], slot2[WAVES], found[2], s_above, s_equal;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t row = SLICED ? a.row0 + blockIdx.y : blockIdx.x;             // (layer * B + b) * Hkv + h
+    const int64_t row = a.row0 + (SLICED ? blockIdx.y : blockIdx.x);           // (layer * B + b) * Hkv + h
     const int slice = SLICED ? blockIdx.x : 0;
     const int h = (int)(row % a.n_kv), b = (int)(row / a.n_kv % a.B);
     const int64_t layer = row / a.n_kv / a.B;
@@ -1196,12 +1196,13 @@ struct CompactArgs {
     float *ks_out, *vs_out, *acc_out;
     const int32_t *cu_tok, *keep_idx, *n_keep;
     int32_t B, n_kv, T_total, n_scales, shift, keep, span;
+    int64_t row0;               // the first head of this launch
 };
 
 __global__ __launch_bounds__(kBlockThreads) void cache_compact_kernel(CompactArgs a) {
     __shared__ __align__(16) float s_top[2][kBlockWaves];     // largest scale of a wave's 8 rows
     const int tid = threadIdx.x, w = tid >> 6, r = tid >> 3, part = (tid & 7) * 16;
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     const int h = (int)(row % a.n_kv), b = (int)(row / a.n_kv % a.B);
     const int64_t head = row / a.n_kv / a.B * a.n_kv + h;
     const bool is_v = blockIdx.y != 0;
@@ -1331,6 +1332,18 @@ hipError_t attend_launch(Ctx* c, const CacheAttendArgs& a, int32_t blocks) {
     return hipGetLastError();
 }
 
+// go(first head, heads) for all heads, by blocks of up to kBlockThreads threads each: a launch may have 2^32 - 1 threads in a dimension.
+constexpr int64_t kHeadsAtOnce = 1 << 21;
+template <typename Go>
+hipError_t by_heads(int64_t heads, const Go& go) {
+    for (int64_t row0 = 0; row0 < heads; row0 += kHeadsAtOnce) {
+        go(row0, (unsigned)(heads - row0 < kHeadsAtOnce ? heads - row0 : kHeadsAtOnce));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
 hipError_t launch_rotary(Ctx* c, int32_t n, const void* q, const void* k, const int32_t* pos, const double* inv_freq, int32_t rot, bool interleaved,
@@ -1438,43 +1451,37 @@ hipError_t launch_cache_evict(Ctx* c, int32_t B, const float* acc, int32_t T_tot
                               int32_t sink, int32_t recent, int32_t* keep_idx, int32_t* n_keep) {
     EvictArgs a{acc, cu_tok, n_tok, B, c->d.n_kv_heads, T_total, max_n, keep, sink, recent, keep_idx, n_keep, 0, 0, c->evict_counts};
     const int64_t heads = (int64_t)c->d.n_layers * B * c->d.n_kv_heads;
-    const dim3 grid((unsigned)heads);
     // as few threads a head as hold its images with eight each, then more images (a load of a row that is none costs as much as one of a row)
     auto whole = [&](auto threads, auto keys) {
         constexpr int N = decltype(threads)::value, K = decltype(keys)::value;
-        hipLaunchKernelGGL((cache_evict_kernel<N, K, false>), grid, dim3(N), 0, c->stream, a);
+        return by_heads(heads, [&](int64_t row0, unsigned here) {
+            a.row0 = row0;
+            hipLaunchKernelGGL((cache_evict_kernel<N, K, false>), dim3(here), dim3(N), 0, c->stream, a);
+        });
     };
     using std::integral_constant;
     constexpr integral_constant<int, 8> k8{};
-    if (max_n <= 8 * 256) {
-        whole(integral_constant<int, 256>{}, k8);
-    } else if (max_n <= 8 * 512) {
-        whole(integral_constant<int, 512>{}, k8);
-    } else if (max_n <= 8 * 1024) {
-        whole(integral_constant<int, 1024>{}, k8);
-    } else if (max_n <= 16 * 1024) {
-        whole(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
-    } else if (max_n <= kEvictSlice) {
-        whole(integral_constant<int, 1024>{}, integral_constant<int, kEvictSlice / 1024>{});
-    } else {
-        // short slices where all of them have room and a place on the chip at once, long ones otherwise, as many heads at a time as there is room for
-        auto go = [&](auto keys) {
-            constexpr int K = decltype(keys)::value;
-            const int slices = (int)(((int64_t)max_n + K * kBlockThreads - 1) / (K * kBlockThreads)), at_once = evict_slices(c->d) / slices;
-            for (a.row0 = 0; a.row0 < heads; a.row0 += at_once) {
-                const unsigned here = (unsigned)(heads - a.row0 < at_once ? heads - a.row0 : at_once);
-                for (a.launch = 0; a.launch < 4; ++a.launch) {
-                    hipLaunchKernelGGL((cache_evict_kernel<kBlockThreads, K, true>), dim3(slices, here), dim3(kBlockThreads), 0, c->stream, a);
-                    const hipError_t e = hipGetLastError();
-                    if (e != hipSuccess) return e;
-                }
+    if (max_n <= 8 * 256) return whole(integral_constant<int, 256>{}, k8);
+    if (max_n <= 8 * 512) return whole(integral_constant<int, 512>{}, k8);
+    if (max_n <= 8 * 1024) return whole(integral_constant<int, 1024>{}, k8);
+    if (max_n <= 16 * 1024) return whole(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+    if (max_n <= kEvictSlice) return whole(integral_constant<int, 1024>{}, integral_constant<int, kEvictSlice / 1024>{});
+    // short slices where all of them have room and a place on the chip at once, long ones otherwise, as many heads at a time as there is room for
+    auto go = [&](auto keys) {
+        constexpr int K = decltype(keys)::value;
+        const int slices = (int)(((int64_t)max_n + K * kBlockThreads - 1) / (K * kBlockThreads)), at_once = evict_slices(c->d) / slices;
+        for (a.row0 = 0; a.row0 < heads; a.row0 += at_once) {
+            const unsigned here = (unsigned)(heads - a.row0 < at_once ? heads - a.row0 : at_once);
+            for (a.launch = 0; a.launch < 4; ++a.launch) {
+                hipLaunchKernelGGL((cache_evict_kernel<kBlockThreads, K, true>), dim3(slices, here), dim3(kBlockThreads), 0, c->stream, a);
+                const hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
             }
-            return hipSuccess;
-        };
-        const int64_t few = heads * (((int64_t)max_n + 8 * kBlockThreads - 1) / (8 * kBlockThreads));
-        return few <= evict_slices(c->d) && few <= c->n_cu ? go(k8) : go(integral_constant<int, kEvictSlice / kBlockThreads>{});
-    }
-    return hipGetLastError();
+        }
+        return hipSuccess;
+    };
+    const int64_t few = heads * (((int64_t)max_n + 8 * kBlockThreads - 1) / (8 * kBlockThreads));
+    return few <= evict_slices(c->d) && few <= c->n_cu ? go(k8) : go(integral_constant<int, kEvictSlice / kBlockThreads>{});
 }
 
 hipError_t launch_cache_compact(Ctx* c, int32_t B, const void* K, const void* V, const float* ks, const float* vs, const float* acc, int32_t T_total, int32_t block,
@@ -1490,10 +1497,12 @@ hipError_t launch_cache_compact(Ctx* c, int32_t B, const void* K, const void* V,
         span = (int32_t)round_up((keep + cuts - 1) / cuts, kCompactRows);
         if ((keep + span - 1) / span > 65535) span = (int32_t)round_up((keep + 65534) / 65535, kCompactRows);
     }
-    const CompactArgs a{(const uint8_t*)K, (const uint8_t*)V, ks, vs, acc, (uint8_t*)K_out, (uint8_t*)V_out, ks_out, vs_out, acc_out, cu_tok, keep_idx, n_keep,
-                        B, c->d.n_kv_heads, T_total, T_total / block + B, log2_of(block), keep, span};
-    hipLaunchKernelGGL(cache_compact_kernel, dim3((unsigned)heads, 2, (unsigned)((keep + span - 1) / span)), dim3(kBlockThreads), 0, c->stream, a);
-    return hipGetLastError();
+    CompactArgs a{(const uint8_t*)K, (const uint8_t*)V, ks, vs, acc, (uint8_t*)K_out, (uint8_t*)V_out, ks_out, vs_out, acc_out, cu_tok, keep_idx, n_keep,
+                  B, c->d.n_kv_heads, T_total, T_total / block + B, log2_of(block), keep, span, 0};
+    return by_heads(heads, [&](int64_t row0, unsigned here) {
+        a.row0 = row0;
+        hipLaunchKernelGGL(cache_compact_kernel, dim3(here, 2, (unsigned)((keep + span - 1) / span)), dim3(kBlockThreads), 0, c->stream, a);
+    });
 }
 
 }  // namespace skv

@@ -720,6 +720,30 @@ def test_compact_of_lists_that_do_not_fit_and_without_weights():
     check_cache(to, out)
 
 
+def test_evict_and_compact_of_more_heads_than_one_launch_has_threads_for():
+    """70 layers, 4096 sequences, 15 heads: 4.3 million heads of 1024 threads are more than the 2^32 threads that a launch may have in a dimension.  Two rows a head, the heavier one stays."""
+    L, B, H, block = 70, 4096, 15, 16
+    T = 2 * B
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("needs 8 GB")
+    ctx = skv.Context(skv.Desc(n_layers=L, n_q_heads=H, n_kv_heads=H, kv_dtype=skv.SKV_BF16, max_tokens=T, max_sentences=1, max_budget=1, max_batch=B))
+    g = torch.Generator(device=DEV).manual_seed(0)
+    acc = torch.randint(0, 3, (L, H, B, 2), device=DEV, generator=g).float()
+    which = (acc[..., 1] > acc[..., 0]).int()                                      # [L][H][B]; equal: the lower row
+    cu, n_tok = i32(2 * np.arange(B + 1)), torch.full((L, B, H), 2, dtype=torch.int32, device=DEV)
+    idx, n_keep = torch.full((L, B, H, 1), -3, dtype=torch.int32, device=DEV), torch.full((L, B, H), -3, dtype=torch.int32, device=DEV)
+    ctx.cache_evict(B, acc, T, cu, n_tok, 5000, 1, 0, 0, idx, n_keep)             # (a bound of 5000 rows takes 1024 threads)
+    assert torch.equal(idx[..., 0], which.transpose(1, 2)) and bool((n_keep == 1).all())
+    K, V = (torch.randint(0, 127, (L, H, B, 2, D), device=DEV, generator=g, dtype=torch.uint8) for _ in range(2))
+    ks, vs = (torch.ones(L, H, T // block + B, device=DEV) for _ in range(2))
+    pick = which[..., None].bool()
+    want = [torch.where(pick, x[..., 1, :], x[..., 0, :]) for x in (K, V)] + [acc.max(-1).values]
+    second = K[..., 1, :].clone()
+    ctx.cache_compact(B, K, V, ks, vs, acc, T, block, cu, idx, 1, n_keep, K, V, ks, vs, acc)
+    assert torch.equal(K[..., 0, :], want[0]) and torch.equal(V[..., 0, :], want[1]) and torch.equal(acc[..., 0], want[2])
+    assert torch.equal(K[..., 1, :], second) and bool((ks == 1).all()) and bool((vs == 1).all())
+
+
 # ---- together -------------------------------------------------------------------------------------------------------------
 
 def _loop(dtype, graph):
