@@ -1491,17 +1491,20 @@ hipError_t launch_cache_compact(Ctx* c, int32_t B, const void* K, const void* V,
     const int64_t heads = (int64_t)c->d.n_layers * B * c->d.n_kv_heads;
     // other outputs: rows cut over four blocks a compute unit, two of them at once, in groups of 128 (8 layers x 8 heads, 2048 of 4096 rows: 18.9 us with one, 17.7 with two, 18.5 with
     // four, 21.7 with eight; 16 x 8 x 8192: 117, 108, 107, 105)
-    int32_t span = keep;
+    const int64_t most = keep < T_total ? keep : T_total;     // rows of a list that can be used, however long it is
+    int64_t span = most;
     if (K != K_out) {
         const int64_t cuts = (4 * (int64_t)c->n_cu + 2 * heads - 1) / (2 * heads);
-        span = (int32_t)round_up((keep + cuts - 1) / cuts, kCompactRows);
-        if ((keep + span - 1) / span > 65535) span = (int32_t)round_up((keep + 65534) / 65535, kCompactRows);
+        span = round_up((most + cuts - 1) / cuts, kCompactRows);
+        if ((most + span - 1) / span > 65535) span = round_up((most + 65534) / 65535, kCompactRows);
     }
+    const unsigned spans = (unsigned)((most + span - 1) / span);
+    if (span > most) span = most;                             // in 32 bits again
     CompactArgs a{(const uint8_t*)K, (const uint8_t*)V, ks, vs, acc, (uint8_t*)K_out, (uint8_t*)V_out, ks_out, vs_out, acc_out, cu_tok, keep_idx, n_keep,
-                  B, c->d.n_kv_heads, T_total, T_total / block + B, log2_of(block), keep, span, 0};
+                  B, c->d.n_kv_heads, T_total, T_total / block + B, log2_of(block), keep, (int32_t)span, 0};
     return by_heads(heads, [&](int64_t row0, unsigned here) {
         a.row0 = row0;
-        hipLaunchKernelGGL(cache_compact_kernel, dim3(here, 2, (unsigned)((keep + span - 1) / span)), dim3(kBlockThreads), 0, c->stream, a);
+        hipLaunchKernelGGL(cache_compact_kernel, dim3(here, 2, spans), dim3(kBlockThreads), 0, c->stream, a);
     });
 }
 

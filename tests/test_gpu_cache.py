@@ -744,6 +744,27 @@ def test_evict_and_compact_of_more_heads_than_one_launch_has_threads_for():
     assert torch.equal(K[..., 1, :], second) and bool((ks == 1).all()) and bool((vs == 1).all())
 
 
+@pytest.mark.parametrize("inplace", [False, True])
+def test_compact_of_lists_with_room_for_more_rows_than_there_are(inplace):
+    """`keep` is the length of a list, not of a sequence: 2^31 - 1 entries of one head, of which 70 are used."""
+    keep = 2 ** 31 - 1
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs 20 GB")
+    rng = np.random.RandomState(4)
+    ref, out = filled([0, 200], 1, 1, 32, rng), filled([0, 200], 1, 1, 32, rng)
+    dev = device_cache(ref)
+    to, want = (dev, ref) if inplace else (device_cache(out), out)
+    ctx = context(H=1)
+    idx, n_keep = torch.empty(keep, dtype=torch.int32, device=DEV), torch.zeros(1, 1, 1, dtype=torch.int32, device=DEV)
+    ctx.cache_evict(1, dev["acc"], 200, dev["cu"], i32([[[70]]]), 200, keep, 4, 10, idx, n_keep)
+    assert int(n_keep) == 70 and np.array_equal(idx[:70].cpu().numpy(), np.arange(70))
+    rows = np.sort(rng.permutation(200)[:70])
+    idx[:70] = i32(rows)
+    ref.compact(0, 0, 0, rows, want)
+    ctx.cache_compact(1, dev["K"], dev["V"], dev["ks"], dev["vs"], dev["acc"], 200, 32, dev["cu"], idx, keep, n_keep, to["K"], to["V"], to["ks"], to["vs"], to["acc"])
+    check_cache(to, want)
+
+
 # ---- together -------------------------------------------------------------------------------------------------------------
 
 def _loop(dtype, graph):
