@@ -372,6 +372,8 @@ int skv_cache_append(skv_ctx* ctx, int32_t layer, int32_t B, const void* k, cons
 /* skv_cache_attend: Eq. 3 for one token per sequence over the cache of layer `layer`: over the rows in use (tok_idx NULL) or over listed ones, as skv_select
  * writes them.  out and lse as in skv_attend (they merge with others by skv_merge_lse): no row gives out = 0, lse = -inf.  A NaN logit or one of +inf gives NaN in out,
  * lse and acc_out; a logit of -inf weighs nothing (0 times its value).  Logits, maxima, weights, sums and the products with V are fp32 (queries and weights enter the products in pieces of 8 bits, three of them where they have 24).
+ * Range: a logit is summed over codes before it meets the block's scale, and weights are up to 256 before they are divided by their sum.  So elements of q are to be 2^112 at most in magnitude, and
+ * a head's rows times its largest v_scale 2^110 (values of 2^118 over the number of rows): beyond, finite results may come out as infinities or NaN.  A weight times its v_scale below 2^-126 counts as 0.
  * Results repeat bit for bit.
  * q dev [B][Hq][D] kv_dtype;  out dev [B][Hq][D] fp32;  lse dev [B][Hq] or NULL
  * max_n    >= the largest n_tok (more are not read).  With tok_idx: n_tok counts the entries of a list
@@ -399,7 +401,7 @@ int skv_cache_attend(skv_ctx* ctx, int32_t layer, int32_t B, const void* q, cons
  *
  * skv_cache_compact: row j of a head becomes its row keep_idx[j], j < n_keep, for all layers, with its gathered weight (acc and acc_out, both or neither).  A block's new scale is the
  * largest that its rows had; codes of rows with a smaller one are rounded again as in skv_cache_append.  The outputs have the layout of the inputs, which they may be
- * themselves, all of them (the list must then be ascending, as skv_cache_evict writes it); rows and scales behind n_keep are left as they were.  An entry that is
+ * themselves, all of them (an entry that is a row must then lie at or behind its own place in the list, as in the strictly ascending ones of skv_cache_evict); rows and scales behind n_keep are left as they were.  An entry that is
  * none of the sequence's rows gives a row of zeros.  Asynchronous.
  * Errors: SKV_EINVAL (null / misaligned pointers, B < 1, T_total < 1, block, keep < 0, acc without acc_out or the other way round, some outputs that are their inputs and some that are
  * not), SKV_ECAPACITY (B > max_batch, T_total > max_tokens).  keep == 0 is a no-op. */

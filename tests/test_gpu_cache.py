@@ -612,6 +612,33 @@ def test_gathered_weights_of_large_logits_add_up(max_n):
             assert abs(total - 4.0) <= 4.0 * (n[b, h] / 32 + 400) * EPS, (b, h, total)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_at_the_ends_of_its_range(dtype):
+    """Elements of a query of 2^112, whose products with codes reach 2^128 nearly; rows times scale of 2^110, with weights of 200 times the reference's before they are divided."""
+    ref = R.Cache([0, 1664], 1, 1, 32)
+    rng, n = np.random.RandomState(0), np.array([[1664]])
+    ref.codes[0] = 0x7e
+    ref.codes[0, 0, 0, 1::3] = 0xfe                            # -448: these rows' weights vanish
+    ref.scale[0] = 2.0 ** -100
+    ref.codes[1] = rng.randint(0, 0x7f, ref.codes[1].shape)
+    dev, ctx = device_cache(ref), context(H=1, G=1, dtype=dtype)
+    q = torch.full((1, 1, D), 2.0 ** 112, dtype=TYPES[dtype], device=DEV)
+    out, lse = run_attend(ref, dev, ctx, 0, q, i32(n), 1664)
+    rows = np.setdiff1d(np.arange(1664), np.arange(1, 1664, 3))
+    want, logit = ref.rows(1, 0, 0, 0, rows).mean(0), 128 * 448 * 2.0 ** 12 / math.sqrt(D)
+    # equal weights, exactly: a sum of them times values, and its quotient; the logit: scale, constant, their products
+    assert np.all(np.abs(out[0, 0] - want) <= (1664 / 32 + 300) * EPS * want) and abs(lse[0, 0] - logit - math.log(len(rows))) <= 8 * EPS * logit
+    # a wave's first tile sets its reference to 0, the others stay 7.65 above it (powers of two) without moving it
+    ref.codes[0] = 0x37                                        # 0.9375
+    ref.codes[0, 0, 0, :128] = 0
+    ref.scale[0], ref.scale[1], ref.codes[1] = 0.5, 2.0 ** 99, 0x7e
+    dev = device_cache(ref)
+    q.fill_(1.0)
+    for max_n in (400000, 1664):                               # 13 tiles a wave, and one
+        out, lse = run_attend(ref, dev, ctx, 0, q, i32(n), max_n)
+        assert np.all(np.abs(out / (448 * 2.0 ** 99) - 1.0) <= (1664 / 32 + 300) * EPS)
+
+
 # ---- evict and compact ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,keep,sink,recent", [(0, 4, 1, 1), (1, 1, 0, 0), (5, 5, 2, 2), (5, 0, 0, 0), (6, 5, 2, 3), (6, 5, 2, 2), (300, 77, 4, 30), (1024, 1023, 0, 0), (1025, 64, 0, 64),
