@@ -639,6 +639,53 @@ def test_attend_at_the_ends_of_its_range(dtype):
         assert np.all(np.abs(out / (448 * 2.0 ** 99) - 1.0) <= (1664 / 32 + 300) * EPS)
 
 
+def attend_on_device(dev, q, n, G, cu, block):
+    """One KV head, in 64 bits on the device: out, lse, the sum of the weights of a row's queries, and the largest sum of |products| of a logit, for each sequence."""
+    for b, m in enumerate(n):
+        rows = torch.arange(m, device=DEV)
+        slot = cu[b] // block + b + rows // block
+        K, V = ((dev[x][0, 0, cu[b]: cu[b] + m].view(torch.float8_e4m3fn).double() * dev[s][0, 0, slot].double()[:, None]) for x, s in (("K", "ks"), ("V", "vs")))
+        x = torch.stack([(q[b, g].double() * K).sum(1) for g in range(G)]) / math.sqrt(D)
+        top = x.max(1, keepdim=True).values
+        e = torch.exp(x - top)
+        z = e.sum(1, keepdim=True)
+        p = e / z
+        size = torch.stack([(p[g][:, None] * V.abs()).sum(0) for g in range(G)])
+        l1 = max(float((q[b, g].double().abs() * K.abs()).sum(1).max()) for g in range(G)) / math.sqrt(D)
+        yield torch.stack([(p[g][:, None] * V).sum(0) for g in range(G)]), (top + torch.log(z))[:, 0], p.sum(0), size, l1
+
+
+@pytest.mark.parametrize("G,dtype", [(1, "bf16"), (8, "bf16"), (2, "f32"), (8, "f32")])
+@pytest.mark.parametrize("n,max_n", [((3001,), 400000), ((1664,), 400000), ((420001, 400777), 420001)])
+def test_gathered_weights_of_more_tiles_than_a_wave_keeps(n, max_n, G, dtype):
+    """A wave keeps the scores of 8 tiles before it writes them: 13 tiles in chunks of 1664 rows (one sequence whose bound is 400000 rows), 8 to 13 in shares of 820000 rows."""
+    rng = np.random.RandomState(G)
+    cu = np.concatenate([[0], np.cumsum(np.array(n) + 3)])
+    T, block = int(cu[-1]), 64
+    g = torch.Generator(device=DEV).manual_seed(G)
+    dev = {x: torch.randint(0, 0x7f, (1, 1, T, D), device=DEV, generator=g, dtype=torch.uint8) | (torch.randint(0, 2, (1, 1, T, D), device=DEV, generator=g, dtype=torch.uint8) << 7)
+           for x in ("K", "V")}
+    dev.update({x: torch.exp2(torch.randint(-10, -5, (1, 1, T // block + len(n)), device=DEV, generator=g).float()) for x in ("ks", "vs")}, cu=i32(cu))
+    dev["acc"] = torch.rand(1, 1, T, device=DEV, generator=g)
+    ctx = context(H=1, G=G, dtype=dtype)
+    ref = R.Cache([0, 1], 1, 1, block)
+    ref.T = T
+    q = torch.from_numpy(rng.standard_normal((len(n), G, D))).to(TYPES[dtype]).to(DEV)
+    acc_out = torch.full((1, 1, T), -1.0, device=DEV)
+    out, lse = run_attend(ref, dev, ctx, 0, q, i32(np.array(n)[:, None]), max_n, acc=dev["acc"], acc_out=acc_out, decay=0.5)
+    for b, (want, wl, p, size, l1) in enumerate(attend_on_device(dev, q, n, G, cu, block)):
+        logit = 388 * EPS * l1
+        # sums of a wave's rows one by one: 128 rows a step of four waves' 32, at most 820000 / 512 of them in a block's share, or 1664
+        w = 2 * logit + 8 * EPS * float(wl.abs().max()) + 8 * EPS + (1700 / 16 + 1200) * EPS
+        assert np.all(np.abs(out[b] - f64(want)) <= 2 * w * f64(size) + 1e-30)
+        assert np.all(np.abs(lse[b] - f64(wl)) <= logit + w + 4 * EPS * np.abs(f64(wl)))
+        at = slice(int(cu[b]), int(cu[b]) + n[b])
+        sure = 0.5 * dev["acc"][0, 0, at].double() + p
+        # decay * acc, and G weights added to it one by one: G + 1 roundings of numbers up to the sum, half a step each
+        assert bool(((acc_out[0, 0, at].double() - sure).abs() <= p * 2 * w + (G + 1) * EPS * sure).all())
+        assert bool((acc_out[0, 0, at.stop: int(cu[b + 1])] == -1.0).all())
+
+
 # ---- evict and compact ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,keep,sink,recent", [(0, 4, 1, 1), (1, 1, 0, 0), (5, 5, 2, 2), (5, 0, 0, 0), (6, 5, 2, 3), (6, 5, 2, 2), (300, 77, 4, 30), (1024, 1023, 0, 0), (1025, 64, 0, 64),
