@@ -125,6 +125,35 @@ def test_rotary_sines_near_half_a_turn(interleaved, rot):
         assert np.all(np.abs(got - want[:, None]) <= 6 * EPS * np.abs(want[:, None])), (np.abs(got / want[:, None] - 1)).max()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [126, 128])
+@pytest.mark.parametrize("n", [4099, 8209])
+def test_rotary_of_prompts_whose_waves_take_several_groups_of_heads(n, rot, interleaved, dtype):
+    """45 heads: two waves a token take 24 and 21 of them, or one takes all, in groups of 4 or 8 with the next group on its way."""
+    H, G = 5, 8
+    ctx = context(H=H, G=G, dtype=dtype)
+    g = torch.Generator(device=DEV).manual_seed(rot + n)
+    q, k = (torch.randn(n, h, D, device=DEV, generator=g).to(TYPES[dtype]) for h in (H * G, H))
+    pos = torch.randint(0, 1 << 20, (n,), device=DEV, generator=g, dtype=torch.int32)
+    freq = skv.rotary_freqs(rot, 500000.0)[0].to(DEV)
+    qo, ko = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
+    ctx.rotary(n, q, k, pos, freq, rot, interleaved, 1.25, qo, ko)
+    angle = pos.double()[:, None] * freq
+    c, s = 1.25 * torch.cos(angle)[:, None], 1.25 * torch.sin(angle)[:, None]
+    at = torch.arange(rot // 2, device=DEV)
+    a, b = (2 * at, 2 * at + 1) if interleaved else (at, at + rot // 2)
+    for x, got in ((q, qo), (k, ko)):
+        x = x.double()
+        want = x.clone()
+        want[..., a], want[..., b] = x[..., a] * c - x[..., b] * s, x[..., b] * c + x[..., a] * s
+        # the bound of test_rotary at 2^20
+        bound = x[..., :rot].abs().amax(-1, keepdim=True) * 2 * 1.25 * (2 * math.pi * 2.0 ** -31 + 2.0 ** -23.3 + 2.0 ** -22 + 4 * EPS) + (want.abs() * 2.0 ** -8 if dtype == "bf16" else 0.0)
+        assert bool(((got.double() - want).abs() <= bound)[..., :rot].all()) and torch.equal(got[..., rot:].double(), x[..., rot:])
+    ctx.rotary(n, q, k, pos, freq, rot, interleaved, 1.25, q, k)                   # where they lie
+    assert torch.equal(q, qo) and torch.equal(k, ko)
+
+
 # ---- append ---------------------------------------------------------------------------------------------------------------
 
 def device_cache(ref):
@@ -837,6 +866,42 @@ def test_compact_of_lists_with_room_for_more_rows_than_there_are(inplace):
     ref.compact(0, 0, 0, rows, want)
     ctx.cache_compact(1, dev["K"], dev["V"], dev["ks"], dev["vs"], dev["acc"], 200, 32, dev["cu"], idx, keep, n_keep, to["K"], to["V"], to["ks"], to["vs"], to["acc"])
     check_cache(to, want)
+
+
+@pytest.mark.parametrize("n", [2047, 2048, 2049, 4095, 4096, 4097, 8191, 8192, 8193, 16383, 16384, 16385, 32767, 32768])
+@pytest.mark.parametrize("kind", ["spread", "ties"])
+def test_evict_at_the_lengths_where_its_blocks_change(n, kind):
+    """256, 512 and 1024 threads of 8 images each, then 16 and 32 images."""
+    rng = np.random.RandomState(n)
+    H, keep, sink, recent = 3, n // 3, 4, n // 10
+    acc = rng.standard_normal((1, H, n)).astype(np.float32)
+    if kind == "ties":
+        acc = np.round(acc)
+    n_tok = np.array([n, n - 1, n // 2])
+    idx, n_keep = torch.full((1, 1, H, keep), -3, dtype=torch.int32, device=DEV), torch.full((1, 1, H), -3, dtype=torch.int32, device=DEV)
+    context(H=H).cache_evict(1, torch.from_numpy(acc).to(DEV), n, i32([0, n]), i32(n_tok[None, None]), n, keep, sink, recent, idx, n_keep)
+    for h in range(H):
+        want = R.evict(acc[0, h, : n_tok[h]], keep, sink, recent)
+        assert int(n_keep[0, 0, h]) == len(want) and np.array_equal(idx[0, 0, h, : len(want)].cpu().numpy(), want), h
+
+
+@pytest.mark.parametrize("block", [16, 128])
+def test_compact_of_many_heads_in_groups(block):
+    """64 heads to another cache: a block takes 384 rows, three groups of 128 with the next one on its way, the last ones fewer."""
+    rng = np.random.RandomState(block)
+    L, H, B, n, keep = 8, 4, 2, 2700, 2500
+    ref, out = filled([0, n + 5, 2 * n + 7], L, H, block, rng), filled([0, n + 5, 2 * n + 7], L, H, block, rng)
+    dev, to = device_cache(ref), device_cache(out)
+    idx, n_keep = np.full((L, B, H, keep), -9, np.int32), np.zeros((L, B, H), np.int32)
+    for l in range(L):
+        for b in range(B):
+            for h in range(H):
+                m = keep - 131 * ((l + b + h) % 5)
+                idx[l, b, h, :m], n_keep[l, b, h] = np.sort(rng.permutation(n)[:m]), m
+                ref.compact(l, b, h, idx[l, b, h, :m], out)
+    ctx = context(L=L, H=H)
+    ctx.cache_compact(B, dev["K"], dev["V"], dev["ks"], dev["vs"], dev["acc"], ref.T, block, dev["cu"], i32(idx), keep, i32(n_keep), to["K"], to["V"], to["ks"], to["vs"], to["acc"])
+    check_cache(to, out)
 
 
 # ---- together -------------------------------------------------------------------------------------------------------------
