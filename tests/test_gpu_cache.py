@@ -992,6 +992,49 @@ def test_a_loop_of_all_of_them_and_its_replay(dtype):
     assert all(torch.equal(cache[x], cache2[x]) for x in cache)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_graph_made_for_far_more_rows_than_there_are(dtype):
+    """What a program captures once is bounded by its capacity: attention in chunks and with the joining launch, eviction in slices, compaction in place, replayed at a few rows, at none, at unlike
+    counts of heads and at more rows than fit a slice.  Against 64 bits and, bit for bit, the same calls made directly."""
+    H, G, keep, most, rows = 2, 2, 500, 131072, 40000
+    ctx, direct = context(H=H, G=G, dtype=dtype), context(H=H, G=G, dtype=dtype)
+    rng = np.random.RandomState(6)
+    ref = filled([0, rows], 1, H, 32, rng)
+    ref.scale[0] = 2.0 ** -8
+    start, dev, eager = (device_cache(ref) for _ in range(3))
+    n_tok, q = torch.zeros(1, H, dtype=torch.int32, device=DEV), torch.zeros(1, H * G, D, dtype=TYPES[dtype], device=DEV)
+    work = torch.empty(ctx.cache_attend_work_bytes(1, most, True), dtype=torch.uint8, device=DEV)
+
+    def outputs():
+        return (torch.zeros(1, H * G, D, device=DEV), torch.zeros(1, H * G, device=DEV), torch.full((1, 1, H, keep), -3, dtype=torch.int32, device=DEV),
+                torch.zeros(1, 1, H, dtype=torch.int32, device=DEV))
+
+    def calls(ctx, dev, out, lse, idx, n_keep):
+        ctx.cache_attend(0, 1, q, dev["K"], dev["V"], dev["ks"], dev["vs"], rows, 32, dev["cu"], n_tok, None, most, out, lse, dev["acc"], dev["acc"], 0.5, work)
+        ctx.cache_evict(1, dev["acc"], rows, dev["cu"], n_tok, most, keep, 4, 100, idx, n_keep)
+        ctx.cache_compact(1, dev["K"], dev["V"], dev["ks"], dev["vs"], dev["acc"], rows, 32, dev["cu"], idx, keep, n_keep, dev["K"], dev["V"], dev["ks"], dev["vs"], dev["acc"])
+
+    mine, theirs = outputs(), outputs()
+    s = torch.cuda.Stream()
+    ctx.set_stream(s.cuda_stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s), torch.cuda.graph(graph, stream=s):
+        calls(ctx, dev, *mine)
+    for n in ([2000, 1999], [0, 1], [rows, rows - 1], [129, 3000], [0, 0], [32769, 500]):
+        n_tok.copy_(i32([n]))
+        q.copy_(torch.from_numpy(rng.standard_normal(tuple(q.shape))))
+        for x in start:
+            dev[x].copy_(start[x])
+            eager[x].copy_(start[x])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        calls(direct, eager, *theirs)
+        assert all(torch.equal(a, b) for a, b in zip(mine, theirs)) and all(torch.equal(dev[x], eager[x]) for x in dev)
+        check_attend(ref, 0, q, [n], f64(mine[0]), f64(mine[1]))
+        assert mine[3].flatten().tolist() == [min(x, keep) for x in n]
+
+
 def test_selected_rows_and_a_resident_window_meet():
     """skv_select's list over the 8-bit cache, a window over skv_attend, joined by skv_merge_lse: attention over the union."""
     H, G, T, S, W, budget = 2, 4, 640, 40, 50, 200
