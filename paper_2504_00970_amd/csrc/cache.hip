@@ -513,7 +513,7 @@ __global__ __launch_bounds__(kCacheWaves * kWave, cache_places(PIECES, DEAL, WEI
                     for (int p = 0; p < PIECES; ++p) {        // the leading 8 bits of what is left: exact, and three times 8 bits are all of them
                         const uint32_t top = __float_as_uint(x) & 0xffff0000u;
                         qf[p][i][j] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
-                        x = __builtin_fabsf(x) == __builtin_inff() ? 0.0f : x - __uint_as_float(top);      // nothing is left of an infinity (NaN stays: its first piece may be one)
+                        x = p == 0 && __builtin_fabsf(x) == __builtin_inff() ? 0.0f : x - __uint_as_float(top);      // nothing is left of an infinity (NaN stays: its first piece may be one)
                     }
                 }
             }
