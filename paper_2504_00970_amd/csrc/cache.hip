@@ -1277,7 +1277,7 @@ inline int log2_of(int32_t n) { return 31 - __builtin_clz((unsigned)n); }
 // to 8192 rows 41 and 34; 64 sequences of up to 1024 rows (2048) 24 and 27, up to 16384 254 and 211.  With weights half as many: 16 x 4096 rows 37 by chunks and 31 in shares, 64 x
 // 1024 rows 35 and 31, 16 x 2048 (1024) 21 and 26.  And rows a chunk of a batch that is dealt in those, at least.
 // More pairs than kSharePairs take blocks of their own, which are then many and long enough (256 sequences of 1024 rows, 8 heads: 79 us by chunks, 101 in shares; 512 of up to 2048 198 and
-// 246), unless the longest sequence would keep its block busy for longer than the chip takes for all rows (255 of 1024 rows and one of 131072: 925 and 156).
+// 246), unless the longest sequence would keep its block busy for longer than the chip takes for all rows (255 of 1024 rows and one of 131072, no weights: 925 and 159).
 constexpr int kCacheShared = 2048, kCacheRagged = 512;
 constexpr int kGridChunk = 1 << 24;        // rows of a chunk whose bytes a 32-bit offset reaches
 bool skewed(const Ctx* c, int32_t max_n, int32_t T_total) { return (int64_t)max_n * c->n_cu > (int64_t)c->d.n_kv_heads * T_total; }
