@@ -1496,7 +1496,6 @@ hipError_t launch_cache_compact(Ctx* c, int32_t B, const void* K, const void* V,
     if (K != K_out) {
         const int64_t cuts = (4 * (int64_t)c->n_cu + 2 * heads - 1) / (2 * heads);
         span = round_up((most + cuts - 1) / cuts, kCompactRows);
-        if ((most + span - 1) / span > 65535) span = round_up((most + 65534) / 65535, kCompactRows);
     }
     const unsigned spans = (unsigned)((most + span - 1) / span);
     if (span > most) span = most;                             // in 32 bits again
