@@ -154,6 +154,24 @@ def test_rotary_of_prompts_whose_waves_take_several_groups_of_heads(n, rot, inte
     assert torch.equal(q, qo) and torch.equal(k, ko)
 
 
+@pytest.mark.parametrize("rot", [126, 128])
+def test_rotary_of_more_tokens_than_a_grid_has_waves(rot):
+    """2^22 blocks of four waves are a token each; behind them waves take a second one, with the angles of its own position."""
+    n = (1 << 24) + 4099
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    ctx = skv.Context(skv.Desc(n_layers=1, n_q_heads=1, n_kv_heads=1, kv_dtype=skv.SKV_BF16, max_tokens=n, max_sentences=1, max_budget=1, max_batch=1))
+    x = torch.empty(n, 1, D, dtype=torch.bfloat16, device=DEV).normal_(generator=torch.Generator(device=DEV).manual_seed(rot))
+    pos, freq = torch.arange(n, dtype=torch.int32, device=DEV) % 100003, skv.rotary_freqs(rot, 10000.0)[0].to(DEV)
+    out = torch.full_like(x, 7.0)
+    ctx.rotary(n, x, None, pos, freq, rot, False, 1.0, out, None)
+    step = 1 << 20
+    part = torch.empty(step, 1, D, dtype=torch.bfloat16, device=DEV)
+    for at in (0, 5 * step + 3, n - step):                     # a call of these tokens alone, whose waves take one each
+        ctx.rotary(step, x[at: at + step], None, pos[at: at + step].clone(), freq, rot, False, 1.0, part, None)
+        assert torch.equal(out[at: at + step], part)
+
+
 # ---- append ---------------------------------------------------------------------------------------------------------------
 
 def device_cache(ref):
@@ -262,6 +280,35 @@ def test_append_token_by_token_and_what_does_not_fit():
     # more tokens than max_new: the first ones
     run_append(ref, dev, ctx, 0, [[0, 0]] * 3, [2, 2, 2], k, k, i32([[0, 0]] * 3), 200, max_new=2, cu_new=[0, 3, 6, 9])
     check_cache(dev, ref)
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_append_of_more_blocks_than_a_grid_has(block):
+    """65535 launch blocks of 32 rows (or of one scale block of 64) take 2.1 (4.2) million rows of a head: the first ones take rows again behind them."""
+    n, held = 65535 * max(block, 32) + 5003, 5
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GB")
+    T = n + held
+    ctx = skv.Context(skv.Desc(n_layers=1, n_q_heads=1, n_kv_heads=1, kv_dtype=skv.SKV_BF16, max_tokens=T, max_batch=1))
+    g = torch.Generator(device=DEV).manual_seed(block)
+    k, v = (torch.randn(n, 1, D, device=DEV, generator=g).mul_(torch.exp(torch.randn(n, 1, 1, device=DEV, generator=g))).bfloat16() for _ in range(2))
+    K, V = (torch.zeros(1, 1, T, D, dtype=torch.uint8, device=DEV) for _ in range(2))
+    ks, vs = (torch.full((1, 1, T // block + 1), 2.0 ** -9, device=DEV) for _ in range(2))
+    acc = torch.ones(1, 1, T, device=DEV)
+    ctx.cache_append(0, 1, k, v, n, i32([0, n]), n, i32([0, T]), i32([[held]]), K, V, ks, vs, T, block, acc)
+    blocks = -(-T // block)
+    for x, codes, scale in ((k, K, ks), (v, V, vs)):
+        rows = torch.zeros(blocks * block, D, dtype=torch.bfloat16, device=DEV)
+        rows[held: T] = x[:, 0]
+        most = rows.view(blocks, -1).abs().amax(1).double()
+        e = torch.ceil(torch.log2(most / 448.0)).clamp(min=-9.0)                   # (no quotient of bf16 numbers by 448 is near enough to a power of two to be rounded across it but for the powers)
+        want = torch.exp2(e)
+        assert bool((most <= 448.0 * want).all()) and bool(((most > 224.0 * want) | (want == 2.0 ** -9)).all())
+        assert torch.equal(scale[0, 0, :blocks].double()[1:], want[1:]) and float(scale[0, 0, 0]) == max(2.0 ** -9, float(want[0]))
+        lost = (rows.view(blocks, block, D).float() / want[:, None, None].float()).to(torch.float8_e4m3fn).view(torch.uint8).view(-1, D)
+        assert torch.equal(codes[0, 0, held:], lost[held: T]) and int(codes[0, 0, :held].max()) == 0
+        del rows, lost
+    assert bool((acc[0, 0, held:] == 0).all()) and bool((acc[0, 0, :held] == 1).all())
 
 
 # ---- attend ---------------------------------------------------------------------------------------------------------------
@@ -715,6 +762,26 @@ def test_gathered_weights_of_more_tiles_than_a_wave_keeps(n, max_n, G, dtype):
         assert bool((acc_out[0, 0, at.stop: int(cu[b + 1])] == -1.0).all())
 
 
+@pytest.mark.parametrize("lengths,listed", [((60000,), 40000), ((60000, 57000), 50000)])
+@pytest.mark.parametrize("G,dtype", [(2, "bf16"), (8, "f32")])
+def test_attend_long_lists(lengths, listed, G, dtype):
+    """Chunks of 256 entries, and of 1024, the most that a block takes; more parts than the attention launch joins."""
+    H = 1 if len(lengths) == 1 else 3
+    rng, ref, dev, ctx, q = attend_case(listed + G, lengths, H, G, dtype, 64, L=1)
+    B = len(lengths)
+    idx, n = np.full((B, H, listed), -5, np.int32), np.zeros((B, H), np.int32)
+    for b in range(B):
+        for h in range(H):
+            n[b, h] = (listed, listed - 1023, 700)[h]
+            idx[b, h, : n[b, h]] = rng.permutation(lengths[b])[: n[b, h]]
+            idx[b, h, : n[b, h]: 7] = rng.choice([-1, 2 ** 31 - 1, 0, lengths[b] - 1], len(range(0, n[b, h], 7)))
+    idx[0, 0, 2048: 4096] = -1                                  # whole blocks of entries that are none
+    out, lse = run_attend(ref, dev, ctx, 0, q, i32(n), listed, idx=i32(idx))
+    check_attend(ref, 0, q, n, out, lse, idx)
+    again = run_attend(ref, dev, ctx, 0, q, i32(n), listed, idx=i32(idx))
+    assert np.array_equal(out, again[0]) and np.array_equal(lse, again[1])
+
+
 # ---- evict and compact ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,keep,sink,recent", [(0, 4, 1, 1), (1, 1, 0, 0), (5, 5, 2, 2), (5, 0, 0, 0), (6, 5, 2, 3), (6, 5, 2, 2), (300, 77, 4, 30), (1024, 1023, 0, 0), (1025, 64, 0, 64),
@@ -1124,6 +1191,45 @@ def test_attend_of_one_long_sequence_among_more_pairs_than_take_shares():
     want[0, 1, 5:7] = 448.0 / rows
     # a lane of a wave adds up its rows' weights of 1 one by one, exactly up to 2^24; then waves and parts
     assert np.all(np.abs(got - want) <= 400 * EPS * want)
+
+
+def test_two_contexts_at_once():
+    """Two streams, a context each: parts and their arrivals, shares, slices of an eviction and compactions in place side by side give what each gives alone."""
+    H, G, most = 2, 4, 40000
+    rng = np.random.RandomState(3)
+    ref = filled([0, 30000, 70000], 1, H, 32, rng)
+    ref.scale[0] = 2.0 ** -8
+    q = torch.from_numpy(rng.standard_normal((2, H * G, D))).bfloat16().to(DEV)
+    n = [i32([[30000, 5], [33000, 40000]]), i32([[700, 1], [1000, 999]])]
+
+    def make(i, s):
+        ctx, dev = context(H=H, G=G), device_cache(ref)
+        if s is not None:
+            ctx.set_stream(s.cuda_stream)
+        work = torch.empty(ctx.cache_attend_work_bytes(2, most, True), dtype=torch.uint8, device=DEV)
+        outs = [torch.zeros(2, H * G, D, device=DEV) for _ in range(3)]
+        idx, n_keep = torch.zeros(1, 2, H, 600, dtype=torch.int32, device=DEV), torch.zeros(1, 2, H, dtype=torch.int32, device=DEV)
+
+        def go():
+            for out, bound, acc in zip(outs, (most, 1000, most), (None, None, dev["acc"])):
+                ctx.cache_attend(0, 2, q, dev["K"], dev["V"], dev["ks"], dev["vs"], ref.T, 32, dev["cu"], n[i], None, bound, out, None, acc, acc, 0.5, work)
+            ctx.cache_evict(2, dev["acc"], ref.T, dev["cu"], n[i], most, 600, 4, 100, idx, n_keep)
+            ctx.cache_compact(2, dev["K"], dev["V"], dev["ks"], dev["vs"], dev["acc"], ref.T, 32, dev["cu"], idx, 600, n_keep, dev["K"], dev["V"], dev["ks"], dev["vs"], dev["acc"])
+        return go, outs + [idx, n_keep] + list(dev.values())
+
+    alone = [make(i, None) for i in range(2)]
+    for go, _ in alone:
+        for _ in range(5):
+            go()
+        torch.cuda.synchronize()
+    both = [make(i, torch.cuda.Stream()) for i in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for go, _ in both:
+            go()
+    torch.cuda.synchronize()
+    for (_, a), (_, b) in zip(alone, both):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
 def test_calls_follow_the_contexts_stream():
